@@ -449,6 +449,84 @@ ac_status ac_conv2d_wgrad_compressed_collapsed(const ac_conv_desc *desc, const v
  */
 ac_status ac_selftest_bounded_wait(void *workspace, uint64_t limit_cycles, void *stream);
 
+/*
+ * The classifier's loss with its gradients. A training step ends its forward pass in a linear layer over
+ * `classes` classes and a softmax cross entropy; kept for backward, its logits are the largest activation
+ * of a network with many classes. These calls never hold them: the classes are taken in pieces, and
+ * backward forms a piece's gradient from h and w again.
+ *
+ *   l = h w^T + bias        lse_t = log sum_v exp l_tv        loss_t = lse_t - l_t,label(t)
+ *   g_tv = dloss_t (exp(l_tv - lse_t) - [v = label(t)])
+ *   dh = g w                dw = g^T h                        dbias_v = sum_t g_tv
+ *
+ * All matrices are dense, rows contiguous. Products are accumulated in fp32, statistics, lse and loss are
+ * fp32; g is rounded to bf16 once, as an operand of the two gradient products, and each gradient once more
+ * when it is written.
+ *   h      in : [tokens][features], desc->dtype.        w      in : [classes][features], desc->dtype.
+ *   bias   in : [classes], desc->dtype; NULL iff desc->has_bias is 0 (likewise dbias). -inf masks a class.
+ *   labels in : [tokens], int64. A label outside [0, classes) marks a token that does not count: its loss
+ *               and its gradient are zero, whatever dloss holds (its lse is written all the same).
+ *   dloss  in : [tokens], fp32: the gradient with respect to each token's loss (1 / count for a mean).
+ *   loss, lse out (backward: lse in): [tokens], fp32.
+ *   dh, dw, dbias out: OVERWRITTEN, shapes and type of h, w and bias.
+ *   workspace : device scratch. ac_linear_ce_workspace_bytes_min is the least that every call accepts (one
+ *               piece of 64 MB of g, or of 4096 classes where that is more, and dh in fp32);
+ *               ac_linear_ce_workspace_bytes has room for g over all classes where that takes 2 GiB at most.
+ *               With any size between, the widest pieces that fit are used: fewer pieces are faster.
+ * ac_linear_ce_step is forward and backward in one call for callers that know dloss beforehand; it saves
+ * one product over the last piece (over everything, where there is one piece). Results are deterministic.
+ * dtype AC_F32 is not built (AC_ERR_UNSUPPORTED). All pointers 16-byte aligned. ac_workspace_status applies.
+ */
+typedef struct {
+    int32_t tokens, classes, features;
+    int32_t dtype;                  /* ac_dtype of h, w, bias and their gradients */
+    int32_t has_bias;               /* 0 or 1 */
+} ac_linear_ce_desc;
+size_t ac_linear_ce_workspace_bytes(const ac_linear_ce_desc *desc);
+size_t ac_linear_ce_workspace_bytes_min(const ac_linear_ce_desc *desc);
+ac_status ac_linear_ce_forward(const ac_linear_ce_desc *desc, const void *h, const void *w, const void *bias,
+                               const int64_t *labels, float *loss, float *lse, void *workspace,
+                               size_t workspace_bytes, void *stream);
+ac_status ac_linear_ce_backward(const ac_linear_ce_desc *desc, const void *h, const void *w, const void *bias,
+                                const int64_t *labels, const float *lse, const float *dloss, void *dh, void *dw,
+                                void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+ac_status ac_linear_ce_step(const ac_linear_ce_desc *desc, const void *h, const void *w, const void *bias,
+                            const int64_t *labels, const float *dloss, float *loss, float *lse, void *dh, void *dw,
+                            void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The update of weight matrices from their gradients: momentum, then orthogonalisation by Newton-Schulz
+ * products, for `batch` matrices of one shape (a weight gradient of this library, [C_out][R*S*C_in] or
+ * [C_out][C_in*R*S], is such a matrix as it lies).
+ *
+ *   v' = momentum v + g       u = g + momentum v' (nesterov) or v'       X = u / (|u|_F + eps)
+ *   `steps` times:  X <- a X + b (X X^T) X + c (X X^T)^2 X
+ *   update = scale X
+ *
+ * The products take fp16 operands and accumulate in fp32; X is carried between the steps with 22 bits (see
+ * the comment in muon.cu on why). X X^T is formed on the shorter side, whichever that is.
+ *   grad         in : [batch][rows][cols], desc->dtype.
+ *   momentum_in  in, momentum_out out: [batch][rows][cols] fp32, v and v'; may be the same pointer. Both NULL:
+ *                     no momentum, u = g.
+ *   update       out: [batch][rows][cols] bf16. The caller applies it, W <- W - rate * update.
+ *   workspace       : device scratch of ac_muon_workspace_bytes(desc) bytes.
+ * A zero gradient gives a zero update (eps must then be positive); infinities and NaN come out as NaN. Each
+ * matrix is normalised and updated by itself. Deterministic. All pointers 16-byte aligned.
+ * ac_workspace_status applies.
+ */
+typedef struct {
+    int32_t batch, rows, cols;
+    int32_t steps;                  /* >= 0 */
+    int32_t dtype;                  /* ac_dtype of grad */
+    int32_t nesterov;               /* 0 or 1 */
+    float momentum;
+    float a, b, c;                  /* the polynomial; 3.4445, -4.7750, 2.0315 is the customary one */
+    float eps, scale;
+} ac_muon_desc;
+size_t ac_muon_workspace_bytes(const ac_muon_desc *desc);
+ac_status ac_muon_update(const ac_muon_desc *desc, const void *grad, const float *momentum_in, float *momentum_out,
+                         void *update, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static, human-readable name of a status code. */
 const char *ac_status_string(ac_status status);
 

@@ -40,6 +40,15 @@ class ac_plan_info(ctypes.Structure):
         "smem_bytes", "tmem_columns", "units_per_cta", "block_n", "a_cells", "phases")]
 
 
+class ac_linear_ce_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "classes", "features", "dtype", "has_bias")]
+
+
+class ac_muon_desc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "rows", "cols", "steps", "dtype", "nesterov")]
+                + [(n, ctypes.c_float) for n in ("momentum", "a", "b", "c", "eps", "scale")])
+
+
 class AcError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -107,6 +116,16 @@ def lib() -> ctypes.CDLL:
         L.ac_compress_rect.argtypes = [dp, i32, i32, vp, vp, vp, vp]
         L.ac_conv2d_wgrad_compressed_rect.restype = ctypes.c_int
         L.ac_conv2d_wgrad_compressed_rect.argtypes = [dp, i32, i32, vp, vp, vp, vp, sz, vp]
+        cp = ctypes.POINTER(ac_linear_ce_desc)
+        for f in (L.ac_linear_ce_workspace_bytes, L.ac_linear_ce_workspace_bytes_min):
+            f.restype, f.argtypes = sz, [cp]
+        for f, pointers in ((L.ac_linear_ce_forward, 7), (L.ac_linear_ce_backward, 10), (L.ac_linear_ce_step, 11)):
+            f.restype, f.argtypes = ctypes.c_int, [cp] + [vp] * pointers + [sz, vp]
+        mp = ctypes.POINTER(ac_muon_desc)
+        L.ac_muon_workspace_bytes.restype = sz
+        L.ac_muon_workspace_bytes.argtypes = [mp]
+        L.ac_muon_update.restype = ctypes.c_int
+        L.ac_muon_update.argtypes = [mp] + [vp] * 5 + [sz, vp]
         L.ac_status_string.restype = ctypes.c_char_p
         L.ac_status_string.argtypes = [ctypes.c_int]
         _lib = L
@@ -363,3 +382,96 @@ def ac_conv2d_wgrad_compressed_collapsed(desc: ConvDesc, z, dy, dw, workspace, w
                                                     _ptr(workspace), workspace_bytes, _stream(stream))
     if st != AC_OK:
         raise AcError(st, "ac_conv2d_wgrad_compressed_collapsed")
+
+
+@dataclass(frozen=True)
+class LinearCeDesc:
+    """Python mirror of ac_linear_ce_desc (see include/ac.h)."""
+    tokens: int
+    classes: int
+    features: int
+    dtype: str = "bf16"
+    bias: bool = False
+
+    def c(self) -> ac_linear_ce_desc:
+        return ac_linear_ce_desc(self.tokens, self.classes, self.features, _DTYPES[self.dtype], int(self.bias))
+
+
+@dataclass(frozen=True)
+class MuonDesc:
+    """Python mirror of ac_muon_desc (see include/ac.h)."""
+    rows: int
+    cols: int
+    batch: int = 1
+    dtype: str = "f32"
+    steps: int = 5
+    momentum: float = 0.95
+    nesterov: bool = True
+    scale: float = 1.0
+    eps: float = 1e-7
+    coefficients: tuple = (3.4445, -4.7750, 2.0315)
+
+    def c(self) -> ac_muon_desc:
+        return ac_muon_desc(self.batch, self.rows, self.cols, self.steps, _DTYPES[self.dtype], int(self.nesterov),
+                            self.momentum, *self.coefficients, self.eps, self.scale)
+
+
+def _bytes(workspace, workspace_bytes):
+    return workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+
+
+def ac_linear_ce_workspace_bytes(desc: LinearCeDesc) -> int:
+    c = desc.c()
+    return int(lib().ac_linear_ce_workspace_bytes(ctypes.byref(c)))
+
+
+def ac_linear_ce_workspace_bytes_min(desc: LinearCeDesc) -> int:
+    c = desc.c()
+    return int(lib().ac_linear_ce_workspace_bytes_min(ctypes.byref(c)))
+
+
+def ac_linear_ce_forward(desc: LinearCeDesc, h, w, bias, labels, loss, lse, workspace, workspace_bytes=None,
+                         stream=None) -> None:
+    """Per-token loss and log-sum-exp of the linear classifier; bias may be None."""
+    c = desc.c()
+    st = lib().ac_linear_ce_forward(ctypes.byref(c), _ptr(h), _ptr(w), _ptr(bias), _ptr(labels), _ptr(loss), _ptr(lse),
+                                    _ptr(workspace), _bytes(workspace, workspace_bytes), _stream(stream))
+    if st != AC_OK:
+        raise AcError(st, "ac_linear_ce_forward")
+
+
+def ac_linear_ce_backward(desc: LinearCeDesc, h, w, bias, labels, lse, dloss, dh, dw, dbias, workspace,
+                          workspace_bytes=None, stream=None) -> None:
+    """Gradients of sum(dloss * loss) from the stored log-sum-exp; bias and dbias may both be None."""
+    c = desc.c()
+    st = lib().ac_linear_ce_backward(ctypes.byref(c), _ptr(h), _ptr(w), _ptr(bias), _ptr(labels), _ptr(lse), _ptr(dloss),
+                                     _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace),
+                                     _bytes(workspace, workspace_bytes), _stream(stream))
+    if st != AC_OK:
+        raise AcError(st, "ac_linear_ce_backward")
+
+
+def ac_linear_ce_step(desc: LinearCeDesc, h, w, bias, labels, dloss, loss, lse, dh, dw, dbias, workspace,
+                      workspace_bytes=None, stream=None) -> None:
+    """Forward and backward in one call, for a dloss that is known beforehand."""
+    c = desc.c()
+    st = lib().ac_linear_ce_step(ctypes.byref(c), _ptr(h), _ptr(w), _ptr(bias), _ptr(labels), _ptr(dloss), _ptr(loss),
+                                 _ptr(lse), _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace),
+                                 _bytes(workspace, workspace_bytes), _stream(stream))
+    if st != AC_OK:
+        raise AcError(st, "ac_linear_ce_step")
+
+
+def ac_muon_workspace_bytes(desc: MuonDesc) -> int:
+    c = desc.c()
+    return int(lib().ac_muon_workspace_bytes(ctypes.byref(c)))
+
+
+def ac_muon_update(desc: MuonDesc, grad, momentum_in, momentum_out, update, workspace, workspace_bytes=None,
+                   stream=None) -> None:
+    """Momentum and the orthogonalised bf16 update; momentum_in may be momentum_out, or both None."""
+    c = desc.c()
+    st = lib().ac_muon_update(ctypes.byref(c), _ptr(grad), _ptr(momentum_in), _ptr(momentum_out), _ptr(update),
+                              _ptr(workspace), _bytes(workspace, workspace_bytes), _stream(stream))
+    if st != AC_OK:
+        raise AcError(st, "ac_muon_update")

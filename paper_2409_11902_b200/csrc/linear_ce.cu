@@ -1,0 +1,523 @@
+// The classifier's loss: logits l = h w^T + b of T tokens over V classes, softmax cross entropy, and its gradients,
+// without keeping the logits.
+//
+//   lse_t  = log sum_v exp l_tv            loss_t = lse_t - l_t,y(t)
+//   g_tv   = dloss_t (exp(l_tv - lse_t) - [v = y(t)])
+//   dh = g w       dw = g^T h       db_v = sum_t g_tv
+//
+// The classes are taken in pieces of `width` columns. The logits kernel leaves, per row and per 64 or 128 columns, the
+// maximum m and s = sum exp(l - m), both fp32, and nothing else; a small kernel joins them to lse. The
+// gradient of a piece is formed by a second product over the piece (its epilogue writes g in the inputs' type), from
+// which come the piece's rows of dw and its share of dh (summed over the pieces in fp32). For the last piece the
+// second product is not needed: the logits kernel leaves e = exp(l - m) of that piece as fp16 (11 bits over a range of
+// 2^40 below the maximum of its block of columns), and g = dloss e exp(m - lse) is one pass over the piece. With room for
+// all V columns there is one piece and three products in all, as many as the formulas have.
+#include "mm_core.cuh"
+
+namespace ac {
+
+using namespace mm;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Ce {
+    const __nv_bfloat16* bias;   // or null
+    const long long* labels;
+    float2* stats;               // [ceil(V/128)][T]
+    float* at_label;             // [T]: the label's logit
+    const float* lse;            // [T]
+    const float* dloss;          // [T]
+    __half* e;                   // [T][pitch]: exp(l - m) of the kept piece, or null
+    __nv_bfloat16* g;            // [T][pitch]
+    long long pitch;
+    int tokens, classes;
+    int first;                   // first class of this piece
+    int width;                   // classes of this piece
+    int block;                   // columns that share one (m, s): the half tile of one epilogue warp
+};
+
+__device__ __forceinline__ bool live(long long label, int classes) { return label >= 0 && label < classes; }
+
+// 32 logits of one row from tensor memory; columns past the piece's end read as -inf.
+__device__ __forceinline__ void logits32(const Ce& c, uint32_t taddr, int col, float* x) {
+    uint32_t r[32];
+    tmem_ld32(taddr, r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+    if (c.bias) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (col + j < c.width) x[j] += __bfloat162float(c.bias[c.first + col + j]);
+    }
+    if (col + 32 > c.width) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (col + j >= c.width) x[j] = -INFINITY;
+    }
+}
+
+// Statistics of a row's 128 columns; KEEP: and exp(l - m) as fp16.
+template <bool KEEP>
+struct StatsEpi : Ce {
+    static constexpr bool kWholeRow = true;
+    template <int COLS>
+    __device__ __forceinline__ void row(uint32_t taddr, int t, int col) const {
+        const bool in = t < tokens;
+        const int label = [&] {
+            const long long y = in ? labels[t] : -1;
+            return live(y, classes) && y >= first + col && y < first + col + COLS ? (int)(y - first) : -1;
+        }();
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < COLS; c += 32) {
+            float x[32];
+            logits32(*this, taddr + c, col + c, x);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) top = fmaxf(top, x[j]);
+            if (__any_sync(0xffffffffu, label >= col + c && label < col + c + 32)) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (label == col + c + j) at_label[t] = x[j];
+            }
+        }
+        // a row of -inf alone (the columns past the end, or a row that truly has nothing): s is then 0, not NaN
+        const float shift = top == -INFINITY ? 0.f : top;
+        float sum[4] = {};
+#pragma unroll 1
+        for (int c = 0; c < COLS; c += 32) {
+            float x[32];
+            logits32(*this, taddr + c, col + c, x);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                x[j] = ex2((x[j] - shift) * kLog2e);
+                sum[j & 3] += x[j];
+            }
+            if constexpr (KEEP) {
+                if (in && col + c < pitch) {
+                    // 2^15 times e: what lies 2^29 and more below the block's maximum loses bits, not what matters
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] *= 32768.f;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8)
+                        if (col + c + j < pitch) store8(e + (long long)t * pitch + col + c + j, x + j);
+                }
+            }
+        }
+        if (in && col < width)
+            stats[(long long)((first + col) / COLS) * tokens + t] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+    }
+};
+
+// g of a piece from its logits and the rows' lse.
+struct GradEpi : Ce {
+    static constexpr bool kWholeRow = true;
+    template <int COLS>
+    __device__ __forceinline__ void row(uint32_t taddr, int t, int col) const {
+        const bool in = t < tokens;
+        const long long y = in ? labels[t] : -1;
+        const bool counts = live(y, classes);
+        const float scale = counts ? dloss[t] : 0.f, shift = counts ? lse[t] : 0.f;
+        const int label = counts && y >= first + col && y < first + col + COLS ? (int)(y - first) : -1;
+#pragma unroll 1
+        for (int c = 0; c < COLS; c += 32) {
+            float x[32];
+            logits32(*this, taddr + c, col + c, x);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = counts ? ex2((x[j] - shift) * kLog2e) * scale : 0.f;
+            if (__any_sync(0xffffffffu, label >= col + c && label < col + c + 32)) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (label == col + c + j) x[j] -= scale;
+            }
+            if (in) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8)
+                    if (col + c + j < pitch) store8(g + (long long)t * pitch + col + c + j, x + j);
+            }
+        }
+    }
+};
+
+// A gradient: bf16 to the caller's dense matrix and/or fp32 sums over the pieces.
+struct OutEpi {
+    static constexpr bool kWholeRow = false;
+    __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
+    float* sum;             // [rows][cols], or null
+    int add;                // 1: what earlier pieces left in `sum` is added
+    int rows, cols;
+    __device__ __forceinline__ void apply8(int, int row, int col, float (&v)[8], bool) const {
+        if (row >= rows || col >= cols) return;
+        const long long at = (long long)row * cols + col;
+        if (cols % 8 == 0) {
+            if (add) {
+                const float4 a = *reinterpret_cast<const float4*>(sum + at), b = *reinterpret_cast<const float4*>(sum + at + 4);
+                v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+                v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+            }
+            if (out) {
+                store8(out + at, v);
+            } else {
+                *reinterpret_cast<float4*>(sum + at) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4*>(sum + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        } else {
+            for (int j = 0; j < 8 && col + j < cols; ++j) {
+                const float x = v[j] + (add ? sum[at + j] : 0.f);
+                if (out) out[at + j] = __float2bfloat16(x); else sum[at + j] = x;
+            }
+        }
+    }
+};
+
+// Joins a row's statistics: lse and loss. 32 rows per block; 8 warps share a row's blocks of columns.
+__global__ void __launch_bounds__(256) join_kernel(const float2* stats, int blocks, int tokens, int classes,
+                                                   const long long* labels, const float* at_label, float* lse, float* loss) {
+    __shared__ float2 part[8][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = blockIdx.x * 32 + lane;
+    float m = -INFINITY, s = 0.f;
+    auto add = [&](float2 o) {
+        // NaN in either maximum or sum has to come out: fmaxf drops it, so the sum carries it
+        const float top = fmaxf(m, o.x), keep = top == -INFINITY ? 0.f : top;
+        s = s * ex2((m - keep) * kLog2e) + o.y * ex2((o.x - keep) * kLog2e);
+        m = top;
+    };
+    if (t < tokens) {
+#pragma unroll 4
+        for (int b = warp; b < blocks; b += 8) add(stats[(long long)b * tokens + t]);
+    }
+    part[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp == 0 && t < tokens) {
+        for (int w = 1; w < 8; ++w) add(part[w][lane]);
+        const float l = m + logf(s);
+        lse[t] = l;
+        loss[t] = live(labels[t], classes) ? l - at_label[t] : 0.f;
+    }
+}
+
+// The kept piece: g = dloss exp(l - m) exp(m - lse), in place over e; the label's entry from its own fp32 logit.
+__global__ void __launch_bounds__(256) kept_kernel(Ce c, const float* at_label) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = blockIdx.x, per_row = (int)(c.pitch / 8);
+    const long long y = c.labels[t];
+    const bool counts = live(y, c.classes);
+    const float lse = c.lse[t], dl = counts ? c.dloss[t] : 0.f;
+    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < per_row; i += gridDim.y * blockDim.x) {
+        const int col = i * 8;
+        const long long at = (long long)t * c.pitch + col;
+        float v[8];
+        load8(c.e + at, v);
+        const float m = col < c.width ? c.stats[(long long)((c.first + col) / c.block) * c.tokens + t].x : lse;
+        const float f = m == -INFINITY ? 0.f : ex2((m - lse) * kLog2e) * (1.f / 32768.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = counts && col + j < c.width ? v[j] * f * dl : 0.f;
+        if (counts && y >= c.first + col && y < c.first + col + 8) {
+            const float p = ex2((at_label[t] - lse) * kLog2e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c.first + col + j == y) v[j] = dl * (p - 1.f);
+        }
+        store8(c.g + at, v);
+    }
+}
+
+// db of a piece: column sums of g in fp32, 64 columns per block, rows in a fixed order.
+__global__ void __launch_bounds__(256) column_sum_kernel(const __nv_bfloat16* g, long long pitch, int tokens, int width,
+                                                         __nv_bfloat16* out) {
+    __shared__ float2 part[8][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 64 + lane * 2;
+    float2 s = make_float2(0.f, 0.f);
+    if (col < width) {
+#pragma unroll 4
+        for (int t = warp; t < tokens; t += 8) {
+            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(g + t * pitch + col));
+            s.x += f.x;
+            s.y += f.y;
+        }
+    }
+    part[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && col < width) {
+        for (int w = 1; w < 8; ++w) {
+            s.x += part[w][lane].x;
+            s.y += part[w][lane].y;
+        }
+        out[col] = __float2bfloat16(s.x);
+        if (col + 1 < width) out[col + 1] = __float2bfloat16(s.y);
+    }
+}
+
+// Rows of `d` values copied to rows of `pitch` (a TMA row has to be a multiple of 16 bytes long).
+__global__ void __launch_bounds__(256) pad_kernel(const __nv_bfloat16* src, __nv_bfloat16* dst, long long rows, int d,
+                                                  int pitch) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int per_row = pitch / 8;
+    const long long n = rows * per_row;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
+        const long long r = i / per_row;
+        const int c = (int)(i - r * per_row) * 8;
+        __nv_bfloat16 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < d ? src[r * d + c + j] : __float2bfloat16(0.f);
+        *reinterpret_cast<uint4*>(dst + i * 8) = *reinterpret_cast<const uint4*>(v);
+    }
+}
+
+inline long long up(long long a, long long b) { return (a + b - 1) / b * b; }
+
+struct CePlan {
+    int width, pieces;                      // columns of g held at a time; pieces of the classes
+    int block;                              // columns per entry of the statistics; 128: tiles of CTA pairs
+    long long pitch;
+    size_t off_stats, off_label, off_lse, off_sum, off_h, off_w, off_g, bytes;
+};
+
+bool valid(const ac_linear_ce_desc* d) {
+    return d && d->tokens > 0 && d->classes > 0 && d->features > 0 && d->dtype == AC_BF16 &&
+           (long long)d->classes * d->features < (1ll << 40) && (long long)d->tokens * d->features < (1ll << 40) &&
+           (long long)d->tokens * up(d->classes, 256) < (1ll << 40);
+}
+
+// `width` columns of g at a time.
+CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
+    CePlan p{};
+    int split;
+    const long long T = d.tokens, V = d.classes, D = d.features, Dp = up(D, 8);
+    p.pieces = (int)((V + width - 1) / width);
+    width = up((V + p.pieces - 1) / p.pieces, 256);
+    p.pieces = (int)((V + width - 1) / width);
+    p.width = (int)width;
+    p.pitch = up(width < V ? width : V, 8);
+    size_t at = kStatusBlockBytes;
+    auto take = [&](long long bytes) {
+        const size_t o = at;
+        at += (size_t)up(bytes, 256);
+        return o;
+    };
+    p.block = mm::use_pairs(d.tokens, p.width, D, 1, false, &split) ? 128 : 64;
+    p.off_stats = take((V + p.block - 1) / p.block * T * 8);
+    p.off_label = take(T * 4);
+    if (D != Dp) {
+        p.off_h = take(T * Dp * 2);
+        p.off_w = take(V * Dp * 2);
+    }
+    if (grad) {
+        if (p.pieces > 1) p.off_sum = take(T * D * 4);
+        p.off_g = take(T * p.pitch * 2);
+    }
+    p.bytes = at;
+    return p;
+}
+
+// Least scratch: a piece of 64 MB or 4096 columns, whichever is more. Below that a product over a piece has too few
+// tiles for the GPU, and dh, which is read and written in fp32 once per piece, costs more than the piece's products.
+long long least_width(const ac_linear_ce_desc& d) {
+    long long w = (32ll << 20) / d.tokens / 256 * 256;
+    if (w < 4096) w = 4096;
+    return w < d.classes ? w : d.classes;
+}
+// Ample scratch: all columns of g if they fit 2 GiB.
+long long ample_width(const ac_linear_ce_desc& d) {
+    long long w = (1ll << 30) / d.tokens / 256 * 256;
+    const long long least = least_width(d);
+    if (w < least) w = least;
+    return w < d.classes ? w : d.classes;
+}
+
+// The widest pieces that fit `bytes`.
+bool plan_ce(const ac_linear_ce_desc& d, bool grad, size_t bytes, CePlan* p) {
+    *p = plan_for(d, grad, d.classes);
+    if (!grad || p->bytes <= bytes) return p->bytes <= bytes;
+    const long long least = least_width(d);
+    *p = plan_for(d, grad, least);
+    if (p->bytes > bytes) return false;
+    // least fits; more pieces of at least `least` columns need less room, so the first that fits is the widest
+    for (int pieces = 2; pieces < p->pieces; ++pieces) {
+        const CePlan q = plan_for(d, grad, (d.classes + pieces - 1) / pieces);
+        if (q.bytes <= bytes) {
+            *p = q;
+            return true;
+        }
+    }
+    return true;
+}
+
+struct Args {
+    const ac_linear_ce_desc* d;
+    const void *h, *w, *bias;
+    const int64_t* labels;
+    const float* dloss;
+    float *loss, *lse;
+    void *dh, *dw, *dbias;
+    void* workspace;
+    size_t bytes;
+    cudaStream_t st;
+};
+
+int blocks_for(long long items, int per_block) {
+    const long long n = (items + per_block - 1) / per_block;
+    return (int)(n < kNumSMs * 8 ? n : kNumSMs * 8);
+}
+
+ac_status run_ce(const Args& a, bool forward, bool grad) {
+    const ac_linear_ce_desc& d = *a.d;
+    CePlan p;
+    if (!plan_ce(d, grad, a.bytes, &p)) return AC_ERR_WORKSPACE_TOO_SMALL;
+    char* ws = static_cast<char*>(a.workspace);
+    uint32_t* status = reinterpret_cast<uint32_t*>(ws);
+    const int T = d.tokens, V = d.classes, D = d.features;
+    const long long Dp = up(D, 8);
+    const void *h = a.h, *w = a.w;
+    bool reset = true;
+    if (D != Dp) {
+        __nv_bfloat16 *hp = reinterpret_cast<__nv_bfloat16*>(ws + p.off_h), *wp = reinterpret_cast<__nv_bfloat16*>(ws + p.off_w);
+        AC_CUDA_TRY(launch_after(pad_kernel, dim3(blocks_for(T * Dp / 8, 256)), dim3(256), 0, a.st,
+                                 static_cast<const __nv_bfloat16*>(h), hp, (long long)T, D, (int)Dp));
+        AC_CUDA_TRY(launch_after(pad_kernel, dim3(blocks_for(V * Dp / 8, 256)), dim3(256), 0, a.st,
+                                 static_cast<const __nv_bfloat16*>(w), wp, (long long)V, D, (int)Dp));
+        h = hp;
+        w = wp;
+    }
+    Ce c{};
+    c.bias = static_cast<const __nv_bfloat16*>(a.bias);
+    c.labels = reinterpret_cast<const long long*>(a.labels);
+    c.stats = reinterpret_cast<float2*>(ws + p.off_stats);
+    c.at_label = reinterpret_cast<float*>(ws + p.off_label);
+    c.lse = a.lse;
+    c.dloss = a.dloss;
+    c.tokens = T;
+    c.classes = V;
+    c.pitch = p.pitch;
+    c.block = p.block;
+    c.g = reinterpret_cast<__nv_bfloat16*>(ws + p.off_g);
+
+    auto piece = [&](int i) {
+        c.first = i * p.width;
+        c.width = V - c.first < p.width ? V - c.first : p.width;
+    };
+    auto rows_of_w = [&] { return static_cast<const char*>(w) + (long long)c.first * Dp * 2; };
+    const Operand H{h, D, T, Dp, 1, 0, false};
+    const bool pairs = p.block == 128;
+    ac_status rc;
+    if (forward) {
+        for (int i = 0; i < p.pieces; ++i) {
+            piece(i);
+            const Operand W{rows_of_w(), D, c.width, Dp, 1, 0, false};
+            if (grad && i == p.pieces - 1) {
+                StatsEpi<true> e{c};
+                e.e = reinterpret_cast<__half*>(c.g);
+                rc = launch_shaped<false, false>(pairs, 1, H, W, T, c.width, D, 1, true, false, status, reset, e, a.st);
+            } else {
+                rc = launch_shaped<false, false>(pairs, 1, H, W, T, c.width, D, 1, true, false, status, reset,
+                                                 StatsEpi<false>{c}, a.st);
+            }
+            if (rc != AC_OK) return rc;
+            reset = false;
+        }
+        AC_CUDA_TRY(launch_after(join_kernel, dim3((T + 31) / 32), dim3(256), 0, a.st,
+                                 static_cast<const float2*>(c.stats), (V + p.block - 1) / p.block, T, V, c.labels,
+                                 static_cast<const float*>(c.at_label), a.lse, a.loss));
+    }
+    if (!grad) return AC_OK;
+    for (int i = p.pieces - 1; i >= 0; --i) {
+        piece(i);
+        if (forward && i == p.pieces - 1) {
+            Ce k = c;
+            k.e = reinterpret_cast<__half*>(c.g);
+            AC_CUDA_TRY(launch_after(kept_kernel, dim3(T, (unsigned)((p.pitch + 8191) / 8192)), dim3(256), 0, a.st, k,
+                                     static_cast<const float*>(c.at_label)));
+        } else {
+            const Operand W{rows_of_w(), D, c.width, Dp, 1, 0, false};
+            rc = launch_shaped<false, false>(pairs, 1, H, W, T, c.width, D, 1, true, false, status, reset, GradEpi{c}, a.st);
+            if (rc != AC_OK) return rc;
+            reset = false;
+        }
+        if (a.dbias)
+            AC_CUDA_TRY(launch_after(column_sum_kernel, dim3((c.width + 63) / 64), dim3(256), 0, a.st,
+                                     static_cast<const __nv_bfloat16*>(c.g), p.pitch, T, c.width,
+                                     static_cast<__nv_bfloat16*>(a.dbias) + c.first));
+        {   // rows of dw: g^T h
+            const Operand G{c.g, c.width, T, p.pitch, 1, 0, true}, Ht{h, D, T, Dp, 1, 0, true};
+            const OutEpi e{static_cast<__nv_bfloat16*>(a.dw) + (long long)c.first * D, nullptr, 0, c.width, D};
+            rc = launch<true, true>(G, Ht, c.width, D, T, 1, true, false, status, false, e, a.st);
+            if (rc != AC_OK) return rc;
+        }
+        {   // dh: g w, over this piece
+            const Operand G{c.g, c.width, T, p.pitch, 1, 0, false}, Wt{rows_of_w(), D, c.width, Dp, 1, 0, true};
+            const OutEpi e{i == 0 ? static_cast<__nv_bfloat16*>(a.dh) : nullptr,
+                           p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sum) : nullptr, i != p.pieces - 1, T, D};
+            rc = launch<false, true>(G, Wt, T, D, c.width, 1, true, false, status, false, e, a.st);
+            if (rc != AC_OK) return rc;
+        }
+    }
+    return AC_OK;
+}
+
+ac_status check(const Args& a, bool forward, bool grad) {
+    if (!a.d || a.d->tokens <= 0 || a.d->classes <= 0 || a.d->features <= 0) return AC_ERR_INVALID_ARG;
+    if (a.d->dtype != AC_BF16 && a.d->dtype != AC_F32) return AC_ERR_INVALID_ARG;
+    if (a.d->has_bias != 0 && a.d->has_bias != 1) return AC_ERR_INVALID_ARG;
+    if (a.d->dtype == AC_F32) return AC_ERR_UNSUPPORTED;
+    if (!valid(a.d)) return AC_ERR_INVALID_ARG;
+    if (!a.h || !a.w || !a.labels || !a.lse || !a.workspace) return AC_ERR_INVALID_ARG;
+    if ((a.d->has_bias != 0) != (a.bias != nullptr)) return AC_ERR_INVALID_ARG;
+    if (forward && !a.loss) return AC_ERR_INVALID_ARG;
+    if (grad && (!a.dloss || !a.dh || !a.dw)) return AC_ERR_INVALID_ARG;
+    if (grad && (a.d->has_bias != 0) != (a.dbias != nullptr)) return AC_ERR_INVALID_ARG;
+    const void* all[] = {a.h, a.w, a.bias, a.labels, a.dloss, a.loss, a.lse, a.dh, a.dw, a.dbias, a.workspace};
+    for (const void* q : all)
+        if (!aligned16(q)) return AC_ERR_MISALIGNED;
+    return AC_OK;
+}
+
+}  // namespace
+}  // namespace ac
+
+using namespace ac;
+
+extern "C" {
+
+size_t ac_linear_ce_workspace_bytes(const ac_linear_ce_desc* desc) {
+    return valid(desc) ? plan_for(*desc, true, ample_width(*desc)).bytes : 0;
+}
+
+size_t ac_linear_ce_workspace_bytes_min(const ac_linear_ce_desc* desc) {
+    return valid(desc) ? plan_for(*desc, true, least_width(*desc)).bytes : 0;
+}
+
+ac_status ac_linear_ce_forward(const ac_linear_ce_desc* desc, const void* h, const void* w, const void* bias,
+                               const int64_t* labels, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    const Args a{desc, h, w, bias, labels, nullptr, loss, lse, nullptr, nullptr, nullptr, workspace, workspace_bytes,
+                 static_cast<cudaStream_t>(stream)};
+    const ac_status st = check(a, true, false);
+    return st != AC_OK ? st : run_ce(a, true, false);
+}
+
+ac_status ac_linear_ce_backward(const ac_linear_ce_desc* desc, const void* h, const void* w, const void* bias,
+                                const int64_t* labels, const float* lse, const float* dloss, void* dh, void* dw,
+                                void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    const Args a{desc, h, w, bias, labels, dloss, nullptr, const_cast<float*>(lse), dh, dw, dbias, workspace,
+                 workspace_bytes, static_cast<cudaStream_t>(stream)};
+    const ac_status st = check(a, false, true);
+    return st != AC_OK ? st : run_ce(a, false, true);
+}
+
+ac_status ac_linear_ce_step(const ac_linear_ce_desc* desc, const void* h, const void* w, const void* bias,
+                            const int64_t* labels, const float* dloss, float* loss, float* lse, void* dh, void* dw,
+                            void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    const Args a{desc, h, w, bias, labels, dloss, loss, lse, dh, dw, dbias, workspace, workspace_bytes,
+                 static_cast<cudaStream_t>(stream)};
+    const ac_status st = check(a, true, true);
+    return st != AC_OK ? st : run_ce(a, true, true);
+}
+
+}  // extern "C"

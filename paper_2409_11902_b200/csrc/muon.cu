@@ -1,0 +1,386 @@
+// The update of a weight matrix from its gradient: momentum, then orthogonalisation by Newton-Schulz products.
+//
+//   v' = beta v + g        u = g + beta v' (nesterov) or v'        X = u / (|u|_F + eps)
+//   `steps` times:  A = X X^T (X^T X where there are more rows than columns)
+//                   X <- a X + (b A + c A^2) X
+//   update = scale X
+//
+// The products run on fp16 operands with fp32 sums: after the division by the norm every entry lies in [-1.3, 1.3] and
+// all that the steps form stays below 4, so fp16's range suffices and its 11 bits are worth three more than bf16's.
+// The step is a X plus a correction; what must not be rounded to 11 bits is the X of the term a X, because a rounding
+// of X's large directions leaks into its small ones, which the remaining steps amplify by up to a^steps = 485. X is
+// therefore carried as two fp16 terms (hi + lo, 22 bits); the products read hi alone. On matrices with singular values
+// from 1 down to 1e-4, and on noisy low-rank ones, that keeps the update within 1.1e-3 of the exact one, where carrying
+// hi alone gives 2e-2 and bf16 1e-1. The diagonals of A and P = b A + c A^2, their largest entries, are carried apart in fp32.
+// A and P are symmetric: half of their tiles are computed and written
+// twice.
+#include "mm_core.cuh"
+
+namespace ac {
+
+using namespace mm;
+
+namespace {
+
+constexpr int kNormBlocks = 512;     // partial sums of squares per matrix at most
+
+// Square symmetric results. A = X X^T, or P = b A + c A^2 from the accumulated square of A's off-diagonal part O:
+// with D the diagonal, A^2 = O^2 + D O + O D + D^2. The diagonals go to fp32 vectors, zeros take their place in the fp16
+// matrices.
+struct SymEpi {
+    static constexpr bool kWholeRow = false;
+    const __half* a;      // null: A from the accumulators
+    const float* da;
+    __half* out;
+    float* dout;
+    float b, c;
+    int n;
+    long long pitch;
+    __device__ __forceinline__ void apply8(int batch, int row, int col, float (&v)[8], bool mirror) const {
+        if (row >= n || col >= n) return;
+        const long long base = (long long)batch * n * pitch, at = base + row * pitch + col, line = batch * pitch;
+        if (a) {
+            float x[8];
+            load8(a + at, x);
+            const float d = da[line + row];
+            const float4 e = *reinterpret_cast<const float4*>(da + line + col), f = *reinterpret_cast<const float4*>(da + line + col + 4);
+            const float other[8] = {e.x, e.y, e.z, e.w, f.x, f.y, f.z, f.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = row == col + j ? fmaf(b, d, c * fmaf(d, d, v[j])) : fmaf(b, x[j], c * fmaf(d + other[j], x[j], v[j]));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (row == col + j) {
+                dout[line + row] = v[j];
+                v[j] = 0.f;
+            }
+        store8(out + at, v);
+        if (mirror) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (col + j < n) out[base + (long long)(col + j) * pitch + row] = __float2half(v[j]);
+        }
+    }
+};
+
+// X' = a X + (P X), as two fp16 terms, or the caller's bf16 update in the last step. P's diagonal multiplies X here:
+// the hi term alone while steps remain that would amplify the difference, all of X in the last two.
+template <bool TALL>
+struct StepEpi {
+    static constexpr bool kWholeRow = false;
+    const __half* hi;
+    __half* lo;             // read and written by the same thread
+    __half* hi_out;
+    const float* dp;        // [batch][sym_pitch]
+    __nv_bfloat16* update;  // last step, else null
+    float a, scale, lo_share;
+    int rows, cols;
+    long long pitch, sym_pitch;
+    __device__ __forceinline__ void apply8(int batch, int row, int col, float (&v)[8], bool) const {
+        if (row >= rows || col >= cols) return;
+        const long long at = ((long long)batch * rows + row) * pitch + col;
+        const float* d = dp + batch * sym_pitch;
+        float x[8], y[8], f[8];
+        load8(hi + at, x);
+        load8(lo + at, y);
+        if constexpr (TALL) {
+            const float4 e = *reinterpret_cast<const float4*>(d + col), g = *reinterpret_cast<const float4*>(d + col + 4);
+            f[0] = e.x; f[1] = e.y; f[2] = e.z; f[3] = e.w;
+            f[4] = g.x; f[5] = g.y; f[6] = g.z; f[7] = g.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = d[row];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = fmaf(a, x[j] + y[j], fmaf(f[j], fmaf(lo_share, y[j], x[j]), v[j]));
+        if (update) {
+            const long long to = ((long long)batch * rows + row) * cols + col;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= scale;
+            if (cols % 8 == 0) {
+                store8(update + to, v);
+            } else {
+                for (int j = 0; j < 8 && col + j < cols; ++j) update[to + j] = __float2bfloat16(v[j]);
+            }
+            return;
+        }
+        store8(hi_out + at, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] -= __half2float(__float2half(v[j]));
+        store8(lo + at, v);
+    }
+};
+
+struct Elements {
+    const void* grad;
+    const float* v_in;      // or null: no momentum
+    float* v_out;
+    float* partial;         // [batch][blocks]
+    __half *hi, *lo;        // [batch][rows][pitch]
+    float beta, eps;
+    int nesterov, bf16;
+    int rows, cols;
+    long long pitch;
+    uint32_t* status;
+};
+
+template <int W>
+__device__ __forceinline__ void load_grad(const Elements& e, long long at, float* g) {
+    if (e.bf16) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(e.grad) + at;
+        if constexpr (W == 4) {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
+            const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
+            g[0] = a.x; g[1] = a.y; g[2] = b.x; g[3] = b.y;
+        } else {
+            g[0] = __bfloat162float(*p);
+        }
+    } else {
+        const float* p = static_cast<const float*>(e.grad) + at;
+        if constexpr (W == 4) {
+            const float4 u = *reinterpret_cast<const float4*>(p);
+            g[0] = u.x; g[1] = u.y; g[2] = u.z; g[3] = u.w;
+        } else {
+            g[0] = *p;
+        }
+    }
+}
+template <int W>
+__device__ __forceinline__ void load_f32(const float* p, float* v) {
+    if constexpr (W == 4) {
+        const float4 u = *reinterpret_cast<const float4*>(p);
+        v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
+        v[0] = *p;
+    }
+}
+
+// v' and the block's share of |u|^2. W: elements per access, 4 where rows of the flat array allow it.
+template <int W>
+__global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ Elements e) {
+    __shared__ float part[8];
+    pdl_launch_dependents();
+    pdl_wait();
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) { e.status[0] = 0u; e.status[1] = 0u; }
+    const long long n = (long long)e.rows * e.cols, base = n * blockIdx.y;
+    float sum = 0.f;
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * W; i < n; i += (long long)gridDim.x * 256 * W) {
+        float g[W];
+        load_grad<W>(e, base + i, g);
+        if (e.v_in) {
+            float v[W];
+            load_f32<W>(e.v_in + base + i, v);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                v[j] = e.beta * v[j] + g[j];
+                g[j] = e.nesterov ? fmaf(e.beta, v[j], g[j]) : v[j];
+            }
+            if constexpr (W == 4)
+                *reinterpret_cast<float4*>(e.v_out + base + i) = make_float4(v[0], v[1], v[2], v[3]);
+            else
+                e.v_out[base + i] = v[0];
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum = fmaf(g[j], g[j], sum);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) sum += part[w];
+        e.partial[blockIdx.y * gridDim.x + blockIdx.x] = sum;
+    }
+}
+
+// X = u / (|u| + eps) as hi + lo. Grid (norm blocks, batch): as many blocks as partial sums.
+template <int W>
+__global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ Elements e) {
+    __shared__ float part[8];
+    pdl_launch_dependents();
+    pdl_wait();
+    float sum = 0.f;
+    for (int i = threadIdx.x; i < gridDim.x; i += 256) sum += e.partial[blockIdx.y * gridDim.x + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int w = 0; w < 8; ++w) sum += part[w];
+    const float inv = 1.f / (sqrtf(sum) + e.eps);
+    const long long n = (long long)e.rows * e.cols, base = n * blockIdx.y;
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * W; i < n; i += (long long)gridDim.x * 256 * W) {
+        float g[W];
+        if (e.v_in) {
+            float v[W];
+            load_f32<W>(e.v_out + base + i, v);
+            if (e.nesterov) load_grad<W>(e, base + i, g);
+#pragma unroll
+            for (int j = 0; j < W; ++j) g[j] = e.nesterov ? fmaf(e.beta, v[j], g[j]) : v[j];
+        } else {
+            load_grad<W>(e, base + i, g);
+        }
+        const int row = (int)(i / e.cols), col = (int)(i - (long long)row * e.cols);
+        const long long at = ((long long)blockIdx.y * e.rows + row) * e.pitch + col;
+        if constexpr (W == 4) {
+            float l[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[j] *= inv;
+                l[j] = g[j] - __half2float(__float2half(g[j]));
+            }
+            *reinterpret_cast<uint2*>(e.hi + at) = make_uint2(pack2<__half>(g[0], g[1]), pack2<__half>(g[2], g[3]));
+            *reinterpret_cast<uint2*>(e.lo + at) = make_uint2(pack2<__half>(l[0], l[1]), pack2<__half>(l[2], l[3]));
+        } else {
+            const float x = g[0] * inv;
+            const __half h = __float2half(x);
+            e.hi[at] = h;
+            e.lo[at] = __float2half(x - __half2float(h));
+        }
+    }
+}
+
+// No steps: update = scale X.
+__global__ void __launch_bounds__(256) unstepped_kernel(const __grid_constant__ Elements e, float scale, __nv_bfloat16* update) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long n = (long long)e.rows * e.cols;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const int row = (int)(i / e.cols), col = (int)(i - (long long)row * e.cols);
+        const long long at = ((long long)blockIdx.y * e.rows + row) * e.pitch + col;
+        update[n * blockIdx.y + i] = __float2bfloat16(scale * (__half2float(e.hi[at]) + __half2float(e.lo[at])));
+    }
+}
+
+inline long long up(long long a, long long b) { return (a + b - 1) / b * b; }
+
+struct MuonPlan {
+    int k;                  // min(rows, cols)
+    long long pitch, sym_pitch;
+    int blocks;
+    size_t off_partial, off_hi[2], off_lo, off_a, off_p, off_da, off_dp, bytes;
+};
+
+bool valid(const ac_muon_desc* d) {
+    if (!d || d->batch <= 0 || d->batch > 65535 || d->rows <= 0 || d->cols <= 0 || d->steps < 0) return false;
+    if (d->dtype != AC_F32 && d->dtype != AC_BF16) return false;
+    if (d->nesterov != 0 && d->nesterov != 1) return false;
+    const float f[] = {d->momentum, d->a, d->b, d->c, d->eps, d->scale};
+    for (float x : f)
+        if (!(x - x == 0.f)) return false;      // infinite or NaN
+    if (d->eps < 0.f) return false;
+    return (long long)d->rows * d->cols < (1ll << 36) / d->batch;
+}
+
+MuonPlan plan_muon(const ac_muon_desc& d) {
+    MuonPlan p{};
+    p.k = d.rows < d.cols ? d.rows : d.cols;
+    p.pitch = up(d.cols, 8);
+    p.sym_pitch = up(p.k, 8);
+    const long long n = (long long)d.rows * d.cols;
+    const long long want = (n + 2047) / 2048, most = kNormBlocks / d.batch > 1 ? kNormBlocks / d.batch : 1;
+    p.blocks = (int)(want < most ? want : most);
+    size_t at = kStatusBlockBytes;
+    auto take = [&](long long bytes) {
+        const size_t o = at;
+        at += (size_t)up(bytes, 256);
+        return o;
+    };
+    p.off_partial = take((long long)p.blocks * d.batch * 4);
+    const long long x = (long long)d.batch * d.rows * p.pitch * 2, s = (long long)d.batch * p.k * p.sym_pitch * 2;
+    p.off_hi[0] = take(x);
+    p.off_hi[1] = take(x);
+    p.off_lo = take(x);
+    p.off_a = take(s);
+    p.off_p = take(s);
+    p.off_da = take((long long)d.batch * p.sym_pitch * 4);
+    p.off_dp = take((long long)d.batch * p.sym_pitch * 4);
+    p.bytes = at;
+    return p;
+}
+
+ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, float* v_out, void* update,
+                   void* workspace, cudaStream_t st) {
+    const MuonPlan p = plan_muon(d);
+    char* ws = static_cast<char*>(workspace);
+    uint32_t* status = reinterpret_cast<uint32_t*>(ws);
+    __half* hi[2] = {reinterpret_cast<__half*>(ws + p.off_hi[0]), reinterpret_cast<__half*>(ws + p.off_hi[1])};
+    __half* lo = reinterpret_cast<__half*>(ws + p.off_lo);
+    __half *A = reinterpret_cast<__half*>(ws + p.off_a), *P = reinterpret_cast<__half*>(ws + p.off_p);
+    float *dA = reinterpret_cast<float*>(ws + p.off_da), *dP = reinterpret_cast<float*>(ws + p.off_dp);
+    Elements e{grad, v_in, v_out, reinterpret_cast<float*>(ws + p.off_partial), hi[0], lo, d.momentum, d.eps, d.nesterov,
+               d.dtype == AC_BF16, d.rows, d.cols, p.pitch, status};
+    const dim3 grid(p.blocks, d.batch);
+    // four at a time where no access crosses a row (then the matrices of a batch are aligned as well)
+    if (d.cols % 4 == 0) {
+        AC_CUDA_TRY(launch_after(momentum_kernel<4>, grid, dim3(256), 0, st, e));
+        AC_CUDA_TRY(launch_after(normalise_kernel<4>, grid, dim3(256), 0, st, e));
+    } else {
+        AC_CUDA_TRY(launch_after(momentum_kernel<1>, grid, dim3(256), 0, st, e));
+        AC_CUDA_TRY(launch_after(normalise_kernel<1>, grid, dim3(256), 0, st, e));
+    }
+    if (d.steps == 0) {
+        AC_CUDA_TRY(launch_after(unstepped_kernel, grid, dim3(256), 0, st, e, d.scale, static_cast<__nv_bfloat16*>(update)));
+        return AC_OK;
+    }
+    const bool tall = d.rows > d.cols;
+    const long long x_stride = (long long)d.rows * p.pitch, s_stride = (long long)p.k * p.sym_pitch;
+    for (int i = 0; i < d.steps; ++i) {
+        const __half* X = hi[i & 1];
+        const Operand Xk{X, d.cols, d.rows, p.pitch, d.batch, x_stride, false}, Xt{X, d.cols, d.rows, p.pitch, d.batch, x_stride, true};
+        const Operand Ak{A, p.k, p.k, p.sym_pitch, d.batch, s_stride, false}, Pk{P, p.k, p.k, p.sym_pitch, d.batch, s_stride, false};
+        const SymEpi gram{nullptr, nullptr, A, dA, 0.f, 0.f, p.k, p.sym_pitch}, poly{A, dA, P, dP, d.b, d.c, p.k, p.sym_pitch};
+        ac_status rc = tall ? launch<true, true>(Xt, Xt, p.k, p.k, d.rows, d.batch, false, true, status, false, gram, st)
+                            : launch<false, false>(Xk, Xk, p.k, p.k, d.cols, d.batch, false, true, status, false, gram, st);
+        if (rc == AC_OK) rc = launch<false, false>(Ak, Ak, p.k, p.k, p.k, d.batch, false, true, status, false, poly, st);
+        auto step = [&](auto& e, auto&& go) {
+            e.hi = X;
+            e.lo = lo;
+            e.hi_out = hi[(i + 1) & 1];
+            e.dp = dP;
+            e.update = i + 1 == d.steps ? static_cast<__nv_bfloat16*>(update) : nullptr;
+            e.a = d.a;
+            e.scale = d.scale;
+            e.lo_share = i + 2 >= d.steps ? 1.f : 0.f;
+            e.rows = d.rows;
+            e.cols = d.cols;
+            e.pitch = p.pitch;
+            e.sym_pitch = p.sym_pitch;
+            return go(e);
+        };
+        if (rc == AC_OK && tall) {
+            StepEpi<true> e;
+            rc = step(e, [&](auto& f) { return launch<false, false>(Xk, Pk, d.rows, d.cols, p.k, d.batch, false, false, status, false, f, st); });
+        } else if (rc == AC_OK) {
+            StepEpi<false> e;
+            rc = step(e, [&](auto& f) { return launch<false, true>(Pk, Xt, d.rows, d.cols, p.k, d.batch, false, false, status, false, f, st); });
+        }
+        if (rc != AC_OK) return rc;
+    }
+    return AC_OK;
+}
+
+}  // namespace
+}  // namespace ac
+
+using namespace ac;
+
+extern "C" {
+
+size_t ac_muon_workspace_bytes(const ac_muon_desc* desc) { return valid(desc) ? plan_muon(*desc).bytes : 0; }
+
+ac_status ac_muon_update(const ac_muon_desc* desc, const void* grad, const float* momentum_in, float* momentum_out,
+                         void* update, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!valid(desc)) return AC_ERR_INVALID_ARG;
+    if (!grad || !update || !workspace) return AC_ERR_INVALID_ARG;
+    if ((momentum_in == nullptr) != (momentum_out == nullptr)) return AC_ERR_INVALID_ARG;
+    const void* all[] = {grad, momentum_in, momentum_out, update, workspace};
+    for (const void* q : all)
+        if (!aligned16(q)) return AC_ERR_MISALIGNED;
+    if (workspace_bytes < plan_muon(*desc).bytes) return AC_ERR_WORKSPACE_TOO_SMALL;
+    return run_muon(*desc, grad, momentum_in, momentum_out, update, workspace, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
