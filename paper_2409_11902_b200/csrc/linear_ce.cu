@@ -61,7 +61,9 @@ __device__ __forceinline__ void logits32(const Ce& c, uint32_t taddr, int col, f
 // Statistics of a row's 128 columns; KEEP: and exp(l - m) as fp16.
 template <bool KEEP>
 struct StatsEpi : Ce {
-    static constexpr bool kWholeRow = true;
+    static constexpr bool kWholeRow = true, kMirror = false;
+    template <int R> struct Ops {};
+    template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
     __device__ __forceinline__ void row(uint32_t taddr, int t, int col) const {
         const bool in = t < tokens;
@@ -112,7 +114,9 @@ struct StatsEpi : Ce {
 
 // g of a piece from its logits and the rows' lse.
 struct GradEpi : Ce {
-    static constexpr bool kWholeRow = true;
+    static constexpr bool kWholeRow = true, kMirror = false;
+    template <int R> struct Ops {};
+    template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
     __device__ __forceinline__ void row(uint32_t taddr, int t, int col) const {
         const bool in = t < tokens;
@@ -142,57 +146,78 @@ struct GradEpi : Ce {
 
 // A gradient: bf16 to the caller's dense matrix and/or fp32 sums over the pieces.
 struct OutEpi {
-    static constexpr bool kWholeRow = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kScalar = true;
     __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
-    float* sum;             // [rows][cols], or null
+    float* sum;             // [rows][pitch], or null
     int add;                // 1: what earlier pieces left in `sum` is added
-    int rows, cols;
-    __device__ __forceinline__ void apply8(int, int row, int col, float (&v)[8], bool) const {
-        if (row >= rows || col >= cols) return;
-        const long long at = (long long)row * cols + col;
-        if (cols % 8 == 0) {
+    int rows, cols, pitch;
+    __device__ __forceinline__ bool scalar() const { return out && cols % 8 != 0; }
+    __device__ __forceinline__ void store1(int, int row, int col, float v) const {
+        if (row < rows && col < cols) out[(long long)row * cols + col] = __float2bfloat16(v);
+    }
+    template <int R> struct Ops { float4 x[R][2]; };
+    template <int R>
+    __device__ __forceinline__ void load(Ops<R>& o, int, int row, int step, int col) const {
+        if (!add || col >= cols) return;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (row + i * step < rows) {
+                const float4* q = reinterpret_cast<const float4*>(sum + (long long)(row + i * step) * pitch + col);
+                o.x[i][0] = q[0];
+                o.x[i][1] = q[1];
+            }
+    }
+    template <int R>
+    __device__ __forceinline__ void apply(const Ops<R>& o, int, int row, int step, int col, float (&v)[R][8]) const {
+        if (col >= cols) return;
+#pragma unroll
+        for (int i = 0; i < R; ++i, row += step) {
+            if (row >= rows) return;
             if (add) {
-                const float4 a = *reinterpret_cast<const float4*>(sum + at), b = *reinterpret_cast<const float4*>(sum + at + 4);
-                v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-                v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+                const float4 a = o.x[i][0], b = o.x[i][1];
+                v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
+                v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
             }
-            if (out) {
-                store8(out + at, v);
-            } else {
-                *reinterpret_cast<float4*>(sum + at) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4*>(sum + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-            }
-        } else {
-            for (int j = 0; j < 8 && col + j < cols; ++j) {
-                const float x = v[j] + (add ? sum[at + j] : 0.f);
-                if (out) out[at + j] = __float2bfloat16(x); else sum[at + j] = x;
+            if (!out) {
+                float4* q = reinterpret_cast<float4*>(sum + (long long)row * pitch + col);
+                q[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+                q[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+            } else if (cols % 8 == 0) {
+                store8(out + (long long)row * cols + col, v[i]);
             }
         }
     }
 };
 
-// Joins a row's statistics: lse and loss. 32 rows per block; 8 warps share a row's blocks of columns.
+// Joins a row's statistics: lse and loss. 8 rows per block; 32 threads share a row's blocks of columns.
 __global__ void __launch_bounds__(256) join_kernel(const float2* stats, int blocks, int tokens, int classes,
                                                    const long long* labels, const float* at_label, float* lse, float* loss) {
-    __shared__ float2 part[8][32];
+    __shared__ float2 part[32][8];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = blockIdx.x * 32 + lane;
+    const int r = threadIdx.x & 7, slice = threadIdx.x >> 3, t = blockIdx.x * 8 + r;
     float m = -INFINITY, s = 0.f;
     auto add = [&](float2 o) {
-        // NaN in either maximum or sum has to come out: fmaxf drops it, so the sum carries it
+        // fmaxf drops a NaN maximum; the sum beside it is NaN then and carries it
         const float top = fmaxf(m, o.x), keep = top == -INFINITY ? 0.f : top;
         s = s * ex2((m - keep) * kLog2e) + o.y * ex2((o.x - keep) * kLog2e);
         m = top;
     };
     if (t < tokens) {
-#pragma unroll 4
-        for (int b = warp; b < blocks; b += 8) add(stats[(long long)b * tokens + t]);
+        int b = slice;
+        for (; b + 96 < blocks; b += 128) {
+            float2 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = stats[(long long)(b + 32 * i) * tokens + t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add(x[i]);
+        }
+        for (; b < blocks; b += 32) add(stats[(long long)b * tokens + t]);
     }
-    part[warp][lane] = make_float2(m, s);
+    part[slice][r] = make_float2(m, s);
     __syncthreads();
-    if (warp == 0 && t < tokens) {
-        for (int w = 1; w < 8; ++w) add(part[w][lane]);
+    if (threadIdx.x < 8 && t < tokens) {
+        for (int w = 1; w < 32; ++w) add(part[w][r]);
         const float l = m + logf(s);
         lse[t] = l;
         loss[t] = live(labels[t], classes) ? l - at_label[t] : 0.f;
@@ -277,7 +302,7 @@ struct CePlan {
     int width, pieces;                      // columns of g held at a time; pieces of the classes
     int block;                              // columns per entry of the statistics; 128: tiles of CTA pairs
     long long pitch;
-    size_t off_stats, off_label, off_lse, off_sum, off_h, off_w, off_g, bytes;
+    size_t off_stats, off_label, off_lse, off_sum, off_h, off_w, off_g, off_slices, slice_bytes, bytes;
 };
 
 bool valid(const ac_linear_ce_desc* d) {
@@ -289,7 +314,6 @@ bool valid(const ac_linear_ce_desc* d) {
 // `width` columns of g at a time.
 CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
     CePlan p{};
-    int split;
     const long long T = d.tokens, V = d.classes, D = d.features, Dp = up(D, 8);
     p.pieces = (int)((V + width - 1) / width);
     width = up((V + p.pieces - 1) / p.pieces, 256);
@@ -302,7 +326,7 @@ CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
         at += (size_t)up(bytes, 256);
         return o;
     };
-    p.block = mm::use_pairs(d.tokens, p.width, D, 1, false, &split) ? 128 : 64;
+    p.block = shape(Problem{d.tokens, p.width, D, 1, true, false}, true, 0).pairs ? 128 : 64;
     p.off_stats = take((V + p.block - 1) / p.block * T * 8);
     p.off_label = take(T * 4);
     if (D != Dp) {
@@ -310,8 +334,12 @@ CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
         p.off_w = take(V * Dp * 2);
     }
     if (grad) {
-        if (p.pieces > 1) p.off_sum = take(T * D * 4);
+        if (p.pieces > 1) p.off_sum = take(T * Dp * 4);
         p.off_g = take(T * p.pitch * 2);
+        const size_t dh = scratch_bytes(Problem{d.tokens, d.features, p.width, 1, true, false});
+        const size_t dw = scratch_bytes(Problem{p.width < V ? p.width : (int)V, d.features, T, 1, true, false});
+        p.slice_bytes = dh > dw ? dh : dw;
+        p.off_slices = take((long long)p.slice_bytes);
     }
     p.bytes = at;
     return p;
@@ -376,7 +404,7 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
     const int T = d.tokens, V = d.classes, D = d.features;
     const long long Dp = up(D, 8);
     const void *h = a.h, *w = a.w;
-    bool reset = true;
+    Call call{status, true, ws + p.off_slices, p.slice_bytes, a.st};
     if (D != Dp) {
         __nv_bfloat16 *hp = reinterpret_cast<__nv_bfloat16*>(ws + p.off_h), *wp = reinterpret_cast<__nv_bfloat16*>(ws + p.off_w);
         AC_CUDA_TRY(launch_after(pad_kernel, dim3(blocks_for(T * Dp / 8, 256)), dim3(256), 0, a.st,
@@ -405,24 +433,23 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
     };
     auto rows_of_w = [&] { return static_cast<const char*>(w) + (long long)c.first * Dp * 2; };
     const Operand H{h, D, T, Dp, 1, 0, false};
-    const bool pairs = p.block == 128;
+    const Shape logits{p.block == 128, 1, false};      // one for all pieces: it sets the statistics' block
     ac_status rc;
     if (forward) {
         for (int i = 0; i < p.pieces; ++i) {
             piece(i);
             const Operand W{rows_of_w(), D, c.width, Dp, 1, 0, false};
+            const Problem q{T, c.width, D, 1, true, false};
             if (grad && i == p.pieces - 1) {
                 StatsEpi<true> e{c};
                 e.e = reinterpret_cast<__half*>(c.g);
-                rc = launch_shaped<false, false>(pairs, 1, H, W, T, c.width, D, 1, true, false, status, reset, e, a.st);
+                rc = launch_shaped<false, false>(H, W, q, logits, call, e);
             } else {
-                rc = launch_shaped<false, false>(pairs, 1, H, W, T, c.width, D, 1, true, false, status, reset,
-                                                 StatsEpi<false>{c}, a.st);
+                rc = launch_shaped<false, false>(H, W, q, logits, call, StatsEpi<false>{c});
             }
             if (rc != AC_OK) return rc;
-            reset = false;
         }
-        AC_CUDA_TRY(launch_after(join_kernel, dim3((T + 31) / 32), dim3(256), 0, a.st,
+        AC_CUDA_TRY(launch_after(join_kernel, dim3((T + 7) / 8), dim3(256), 0, a.st,
                                  static_cast<const float2*>(c.stats), (V + p.block - 1) / p.block, T, V, c.labels,
                                  static_cast<const float*>(c.at_label), a.lse, a.loss));
     }
@@ -436,9 +463,8 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
                                      static_cast<const float*>(c.at_label)));
         } else {
             const Operand W{rows_of_w(), D, c.width, Dp, 1, 0, false};
-            rc = launch_shaped<false, false>(pairs, 1, H, W, T, c.width, D, 1, true, false, status, reset, GradEpi{c}, a.st);
+            rc = launch_shaped<false, false>(H, W, Problem{T, c.width, D, 1, true, false}, logits, call, GradEpi{c});
             if (rc != AC_OK) return rc;
-            reset = false;
         }
         if (a.dbias)
             AC_CUDA_TRY(launch_after(column_sum_kernel, dim3((c.width + 63) / 64), dim3(256), 0, a.st,
@@ -446,15 +472,15 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
                                      static_cast<__nv_bfloat16*>(a.dbias) + c.first));
         {   // rows of dw: g^T h
             const Operand G{c.g, c.width, T, p.pitch, 1, 0, true}, Ht{h, D, T, Dp, 1, 0, true};
-            const OutEpi e{static_cast<__nv_bfloat16*>(a.dw) + (long long)c.first * D, nullptr, 0, c.width, D};
-            rc = launch<true, true>(G, Ht, c.width, D, T, 1, true, false, status, false, e, a.st);
+            const OutEpi e{static_cast<__nv_bfloat16*>(a.dw) + (long long)c.first * D, nullptr, 0, c.width, D, 0};
+            rc = launch<true, true>(G, Ht, Problem{c.width, D, T, 1, true, false}, call, e);
             if (rc != AC_OK) return rc;
         }
         {   // dh: g w, over this piece
             const Operand G{c.g, c.width, T, p.pitch, 1, 0, false}, Wt{rows_of_w(), D, c.width, Dp, 1, 0, true};
             const OutEpi e{i == 0 ? static_cast<__nv_bfloat16*>(a.dh) : nullptr,
-                           p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sum) : nullptr, i != p.pieces - 1, T, D};
-            rc = launch<false, true>(G, Wt, T, D, c.width, 1, true, false, status, false, e, a.st);
+                           p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sum) : nullptr, i != p.pieces - 1, T, D, (int)Dp};
+            rc = launch<false, true>(G, Wt, Problem{T, D, c.width, 1, true, false}, call, e);
             if (rc != AC_OK) return rc;
         }
     }

@@ -3,17 +3,20 @@
 // D[b] = A[b] * B[b]^T with A [M x K], B [N x K], 16-bit operands (both fp16 or both bf16), fp32 accumulators in
 // tensor memory. Either operand may lie K-contiguous ("K-major": rows of A as stored) or M/N-contiguous ("MN-major":
 // the transposed matrix as stored), so no product of this library transposes anything in memory. What becomes of the
-// accumulators is the epilogue's business: a functor reads them from tensor memory, 8 consecutive columns of one row
-// at a time, or a whole row of a tile.
+// accumulators is the epilogue's business: a functor gets them 8 consecutive columns of a row at a time,
+// or reads a row's half tile from tensor memory itself (kWholeRow).
 //
 // One CTA per SM, 12 warps: warp 0 loads K-tiles of 64 by TMA into a ring of shared-memory stages (128-byte swizzle),
 // warp 1 issues the MMAs, warp 2 owns the tensor memory, warps 4-11 run the epilogue of one accumulator while the
 // other one is being filled (two accumulators of BN columns). Two shapes:
 //   CG = 2, BN = 256: a pair of SMs computes a 256 x 256 tile (cta_group::2); each holds 128 rows of A and 128 rows
 //           of B, so a K-tile costs 32 KB of shared memory per SM for twice the MMA work of a lone 128 x 128 tile.
-//   CG = 1, BN = 128: 128 x 128 tiles for problems with fewer than a GPU's worth of large tiles. With SPLIT, a cluster
-//           of up to 8 CTAs shares one tile, each a slice of K; the partial sums meet in distributed shared memory
-//           and are added in the order of the slices, so results do not depend on timing.
+//   CG = 1, BN = 128: 128 x 128 tiles for problems with fewer than a GPU's worth of large tiles.
+// Where the tiles are too few and K is long, K is cut into slices: each is a tile of its own that leaves fp32 sums in the
+// workspace, and a second kernel adds the slices in their order and applies the epilogue (a cluster that adds them up in
+// distributed shared memory was slower: that memory gives about 25 GB/s to an SM, the L2 three times as much).
+// K-tiles of 64 arrive at one per 0.27 us and SM for either shape (64 bytes per clock from the L2, or the MMAs of a pair);
+// shape() chooses shape and slices by that rate.
 #pragma once
 
 #include <cuda.h>
@@ -31,33 +34,42 @@ using namespace tc;
 constexpr int kThreads = 384;
 constexpr int kEpiWarps = 8;
 constexpr int kBK = 64;                      // K-tile: one 128-byte swizzle row of 16-bit elements
-constexpr int kStages = 6;
-constexpr int kMaxSplit = 8;
+constexpr int kMaxStages = 6;
+constexpr int kPatchPitch = 36;              // floats between the rows of a warp's 32 x 32 patch: no bank conflicts
+constexpr int kPatchBytes = kEpiWarps * 32 * kPatchPitch * 4;
+constexpr int kMaxSlices = 16;
 
 struct Params {
     int m, n;             // extents of the result
     int ktiles;           // ceil(K / 64)
     int tiles_m, tiles_n;
     int per_batch;        // tiles of one matrix of the batch
-    int tiles;            // per_batch * batch
+    int batch;
+    int slices;           // of K
+    int tiles;            // per_batch * batch * slices
     int group;            // tiles of the fast direction that are cycled before the slow direction advances
     int fast_m;           // 1: tiles of M are the fast direction
-    int sym;              // 1: the result is symmetric; only tiles with tile_n >= tile_m are computed
-    int split;            // CTAs that share a tile's K (SPLIT kernels)
+    int half;             // 1: the result is symmetric; only tiles with tile_n >= tile_m are computed
+    int same;             // 1: B is A, so a tile on the diagonal loads its rows once
     uint32_t idesc;
     uint32_t* status;     // status block of the workspace
     int reset_status;     // 1: first launch of the call
 };
 
 struct Tile {
-    int batch, tm, tn;
+    int batch;            // slice * Params::batch + the matrix
+    int tm, tn;
+    int k0, k1;           // K-tiles
 };
 
 __device__ __forceinline__ Tile decode_tile(const Params& p, int t) {
     Tile r;
     r.batch = t / p.per_batch;
     int i = t - r.batch * p.per_batch;
-    if (p.sym) {
+    const int slice = r.batch / p.batch;
+    r.k0 = (int)((long long)p.ktiles * slice / p.slices);
+    r.k1 = (int)((long long)p.ktiles * (slice + 1) / p.slices);
+    if (p.half) {
         int row = 0;
         while (i >= p.tiles_n - row) { i -= p.tiles_n - row; ++row; }
         r.tm = row;
@@ -87,11 +99,6 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
-}
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
@@ -186,8 +193,7 @@ __device__ __forceinline__ void store8(T* dst, const float* v) {      // dst 16-
     u.w = pack2<T>(v[6], v[7]);
     *reinterpret_cast<uint4*>(dst) = u;
 }
-__device__ __forceinline__ void load8(const __half* src, float* v) {
-    const uint4 u = *reinterpret_cast<const uint4*>(src);
+__device__ __forceinline__ void unpack8(const uint4& u, float* v) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -196,11 +202,12 @@ __device__ __forceinline__ void load8(const __half* src, float* v) {
         v[2 * i + 1] = f.y;
     }
 }
+__device__ __forceinline__ void load8(const __half* src, float* v) { unpack8(*reinterpret_cast<const uint4*>(src), v); }
 
 // ---- the kernel ---------------------------------------------------------------
 
 struct Shared {
-    uint64_t full[kStages], empty[kStages], tfull[2], tempty[2];
+    uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
     uint32_t tmem;
     int abort;
 };
@@ -213,47 +220,108 @@ __device__ __forceinline__ void flag_timeout(int* abort_s, uint32_t* status, uin
 }
 
 template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { return 128 * 128 + BN / CG * 128; }
-template <int CG, int BN> __host__ __device__ constexpr int smem_bytes() { return kStages * stage_bytes<CG, BN>() + 1024; }
+// Five stages where the epilogue needs its patches, six where it works on whole rows.
+template <class Epi> __host__ __device__ constexpr int stage_count() { return Epi::kWholeRow ? kMaxStages : kMaxStages - 1; }
+template <int CG, int BN, class Epi> __host__ __device__ constexpr int smem_bytes() {
+    return stage_count<Epi>() * stage_bytes<CG, BN>() + (Epi::kWholeRow ? 0 : kPatchBytes) + 1024;
+}
 
-// Hands 8 columns of one row at a time to the functor, from tensor memory.
-template <int COLS, class Epi>
-__device__ __forceinline__ void epilogue_by_8(const Epi& epi, uint32_t taddr, int batch, int row, int col, bool mirror) {
-#pragma unroll 1
-    for (int c = 0; c < COLS; c += 32) {
-        uint32_t r[32];
-        tmem_ld32(taddr + c, r);
+// The mirror image of a 32 x 32 patch whose values the warp holds as v: 8 columns at (lane % 4) * 8 of rows lane / 4 + 8 i.
+template <class Epi>
+__device__ __forceinline__ void store_mirror_patch(const Epi& epi, float* patch, int lane, int batch, int row, int col,
+                                                   const float (&v)[4][8]) {
+    const int pr = lane >> 2, pc = (lane & 3) * 8;
+    __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-            float v[8];
+    for (int i = 0; i < 4; ++i) {
+        float* q = patch + (i * 8 + pr) * kPatchPitch + pc;
+        *reinterpret_cast<float4*>(q) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+        *reinterpret_cast<float4*>(q + 4) = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+    }
+    __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[j + i]);
-            epi.apply8(batch, row, col + c + j, v, mirror);
-        }
+    for (int i = 0; i < 4; ++i) {
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = patch[(pc + j) * kPatchPitch + i * 8 + pr];
+        epi.store_mirror(batch, col + i * 8 + pr, row + pc, w);
     }
 }
 
-template <int CG, int BN, bool AMN, bool BMN, bool SPLIT, class Epi>
+// The same values to rows that no 16-byte access fits (a destination with an odd number of columns): one row at a time,
+// the 32 threads side by side.
+template <class Epi>
+__device__ __forceinline__ void store_scalar_patch(const Epi& epi, float* patch, int lane, int batch, int row, int col,
+                                                   const float (&v)[4][8]) {
+    const int pr = lane >> 2, pc = (lane & 3) * 8;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float* q = patch + (i * 8 + pr) * kPatchPitch + pc;
+        *reinterpret_cast<float4*>(q) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+        *reinterpret_cast<float4*>(q + 4) = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+    }
+    __syncwarp();
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r) epi.store1(batch, row + r, col + lane, patch[r * kPatchPitch + lane]);
+}
+
+// Tensor memory gives a thread one row; memory wants the threads of a warp side by side along rows. A warp passes 32 x 32
+// values through a patch of shared memory, after which 4 threads hold 8 columns each of one row: accesses of 64 bytes
+// (16-bit results) on 8 rows at a time. A symmetric result's mirror image is read from the patch by columns. What the
+// functor reads beside the accumulators (`ops`) is requested a patch ahead; the first before the accumulators are waited for.
+template <int COLS, class Epi>
+__device__ __forceinline__ void epilogue_by_patch(const Epi& epi, typename Epi::template Ops<4>& ops, float* patch, uint32_t taddr,
+                                                  int lane, int batch, int row, int col, bool mirror) {
+    const int pr = lane >> 2, pc = (lane & 3) * 8;
+#pragma unroll 2
+    for (int c = 0; c < COLS; c += 32) {
+        uint32_t r[32];
+        tmem_ld32(taddr + c, r);
+        float* own = patch + lane * kPatchPitch;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4)
+            *reinterpret_cast<uint4*>(own + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+        __syncwarp();
+        typename Epi::template Ops<4> now = ops;
+        if (c + 32 < COLS) epi.load(ops, batch, row + pr, 8, col + c + 32 + pc);
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float* q = patch + (i * 8 + pr) * kPatchPitch + pc;
+            const float4 a = *reinterpret_cast<const float4*>(q), b = *reinterpret_cast<const float4*>(q + 4);
+            v[i][0] = a.x; v[i][1] = a.y; v[i][2] = a.z; v[i][3] = a.w;
+            v[i][4] = b.x; v[i][5] = b.y; v[i][6] = b.z; v[i][7] = b.w;
+        }
+        epi.apply(now, batch, row + pr, 8, col + c + pc, v);
+        if constexpr (Epi::kMirror) {
+            if (mirror) store_mirror_patch(epi, patch, lane, batch, row, col + c, v);
+        }
+        if constexpr (Epi::kScalar) {
+            if (epi.scalar()) store_scalar_patch(epi, patch, lane, batch, row, col + c, v);
+        }
+        __syncwarp();
+    }
+}
+
+template <int CG, int BN, bool AMN, bool BMN, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
           const __grid_constant__ Params p, const __grid_constant__ Epi epi) {
-    static_assert(!SPLIT || CG == 1, "a split tile is a cluster of single CTAs");
     constexpr int NB = BN / CG;               // rows of B that one CTA holds
     constexpr uint32_t kStage = stage_bytes<CG, BN>();
-    constexpr bool kCluster = CG == 2 || SPLIT;
+    constexpr int kStages = stage_count<Epi>();
     extern __shared__ uint8_t smem_raw[];
     __shared__ Shared sh;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = kCluster ? cluster_rank() : 0;
-    const int per_tile = SPLIT ? p.split : CG;                       // CTAs of one tile
-    const int unit = blockIdx.x / per_tile, units = gridDim.x / per_tile;
-    const int k_begin = SPLIT ? (int)((long long)p.ktiles * rank / p.split) : 0;
-    const int k_end = SPLIT ? (int)((long long)p.ktiles * (rank + 1) / p.split) : p.ktiles;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
     volatile int* abort_flag = &sh.abort;
 
     if (tid == 0) {
         sh.abort = 0;
-        for (int s = 0; s < kStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int s = 0; s < kMaxStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&sh.tfull[a], 1); mbar_init(&sh.tempty[a], kEpiWarps * CG); }
         fence_barrier_init();
         prefetch_tmap(&ta);
@@ -262,7 +330,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     if (warp == 2) tmem_alloc_cg<CG>(&sh.tmem, 2 * BN);
     tc_fence_before();
     __syncthreads();
-    if constexpr (kCluster) cluster_sync();
+    if constexpr (CG == 2) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     pdl_launch_dependents();
@@ -275,14 +343,17 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     if (warp == 0) {
         // ---------------------------------------------------------------- loads
         if (elect_one()) {
-            pdl_wait();
             int it = 0;
             bool ok = true;
+            Tile tile = decode_tile(p, unit);
+            pdl_wait();
             for (int t = unit; t < p.tiles && ok; t += units) {
-                const Tile tile = decode_tile(p, t);
+                if (t != unit) tile = decode_tile(p, t);
                 const int row0 = tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0);
                 const int col0 = tile.tn * BN + (CG == 2 ? (int)rank * NB : 0);
-                for (int kt = k_begin; kt < k_end; ++kt, ++it) {
+                const bool once = p.same && tile.tm == tile.tn;
+                const int matrix = tile.batch % p.batch;
+                for (int kt = tile.k0; kt < tile.k1; ++kt, ++it) {
                     const int s = it % kStages;
                     if (!mbar_wait(&sh.empty[s], ((it / kStages) & 1) ^ 1, abort_flag)) {
                         flag_timeout(&sh.abort, p.status, 0x1100u + s);
@@ -290,23 +361,24 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
                         break;
                     }
                     // a pair's loads all complete on the leader's barrier; it alone announces the bytes of both
-                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&sh.full[s], kStage * CG);
+                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&sh.full[s], (once ? 128 * 128 : kStage) * CG);
                     uint32_t bar = smem_u32(&sh.full[s]);
                     if constexpr (CG == 2) bar = map_rank(bar, 0);
                     const uint32_t a = base + s * kStage, b = a + 128 * 128;
                     if constexpr (AMN) {
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
-                            tma_load_3d<CG>(a + j * 8192, &ta, bar, row0 + 64 * j, kt * kBK, tile.batch);
+                            tma_load_3d<CG>(a + j * 8192, &ta, bar, row0 + 64 * j, kt * kBK, matrix);
                     } else {
-                        tma_load_3d<CG>(a, &ta, bar, kt * kBK, row0, tile.batch);
+                        tma_load_3d<CG>(a, &ta, bar, kt * kBK, row0, matrix);
                     }
+                    if (once) continue;
                     if constexpr (BMN) {
 #pragma unroll
                         for (int j = 0; j < NB / 64; ++j)
-                            tma_load_3d<CG>(b + j * 8192, &tb, bar, col0 + 64 * j, kt * kBK, tile.batch);
+                            tma_load_3d<CG>(b + j * 8192, &tb, bar, col0 + 64 * j, kt * kBK, matrix);
                     } else {
-                        tma_load_3d<CG>(b, &tb, bar, kt * kBK, col0, tile.batch);
+                        tma_load_3d<CG>(b, &tb, bar, kt * kBK, col0, matrix);
                     }
                 }
             }
@@ -328,7 +400,9 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             }
             tc_fence_after();
             const uint32_t d = tmem + acc * BN;
-            for (int kt = k_begin; kt < k_end; ++kt, ++it) {
+            const Tile tile = decode_tile(p, t);
+            const uint32_t b_off = p.same && tile.tm == tile.tn ? 0 : 128 * 128;
+            for (int kt = tile.k0; kt < tile.k1; ++kt, ++it) {
                 const int s = it % kStages;
                 got = mbar_wait(&sh.full[s], (it / kStages) & 1, abort_flag);
                 if (!__all_sync(0xffffffffu, got)) {
@@ -338,12 +412,12 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
                 }
                 tc_fence_after();
                 const uint32_t a_lo = desc_lo(base + s * kStage, AMN ? 8192 : 16);
-                const uint32_t b_lo = desc_lo(base + s * kStage + 128 * 128, BMN ? 8192 : 16);
+                const uint32_t b_lo = desc_lo(base + s * kStage + b_off, BMN ? 8192 : 16);
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)     // K = 16 each: 32 bytes along a K-major row, 16 rows of an MN-major slab
                     if (leader)
                         mma_words<CG>(d, a_lo + kk * (AMN ? 128 : 2), hi, b_lo + kk * (BMN ? 128 : 2), hi, p.idesc,
-                                      (uint32_t)(kt > k_begin || kk > 0));
+                                      (uint32_t)(kt > tile.k0 || kk > 0));
                 if (leader) commit_cg<CG>(&sh.empty[s]);
                 __syncwarp();
             }
@@ -358,40 +432,33 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         int n = 0;
         for (int t = unit; t < p.tiles; t += units, ++n) {
             const int acc = n & 1;
+            const Tile tile = decode_tile(p, t);
+            const int row = tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) + quarter * 32;
+            const int col = tile.tn * BN + half * (BN / 2);
+            typename Epi::template Ops<4> ops;
+            epi.load(ops, tile.batch, row + (lane >> 2), 8, col + (lane & 3) * 8);
             const bool got = mbar_wait(&sh.tfull[acc], (n >> 1) & 1, abort_flag);
             if (!__all_sync(0xffffffffu, got)) {
                 if (lane == 0) flag_timeout(&sh.abort, p.status, 0x1400u + acc);
                 break;
             }
             tc_fence_after();
-            const Tile tile = decode_tile(p, t);
-            if constexpr (SPLIT) {
-                // partial sums to shared memory, [column][row]; the stages are free once the MMAs are complete
-                float* part = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)));
-#pragma unroll 1
-                for (int c = 0; c < BN / 2; c += 32) {
-                    uint32_t r[32];
-                    tmem_ld32(lanes + acc * BN + c, r);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        part[(half * (BN / 2) + c + j) * 128 + quarter * 32 + lane] = __uint_as_float(r[j]);
-                }
+            if constexpr (Epi::kWholeRow) {
+                epi.template row<BN / 2>(lanes + acc * BN, row + lane, col);
             } else {
-                const int row = tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) + quarter * 32 + lane;
-                const int col = tile.tn * BN + half * (BN / 2);
-                if constexpr (Epi::kWholeRow)
-                    epi.template row<BN / 2>(lanes + acc * BN, row, col);
+                float* patch = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + kStages * kStage) +
+                               (warp - 4) * 32 * kPatchPitch;
+                epilogue_by_patch<BN / 2>(epi, ops, patch, lanes + acc * BN, lane, tile.batch, row, col,
+                                          p.half && tile.tm != tile.tn);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                uint32_t bar = smem_u32(&sh.tempty[acc]);
+                if constexpr (CG == 2)
+                    mbar_arrive_cluster(map_rank(bar, 0));
                 else
-                    epilogue_by_8<BN / 2>(epi, lanes + acc * BN, tile.batch, row, col, p.sym && tile.tm != tile.tn);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    uint32_t bar = smem_u32(&sh.tempty[acc]);
-                    if constexpr (CG == 2)
-                        mbar_arrive_cluster(map_rank(bar, 0));
-                    else
-                        mbar_arrive(&sh.tempty[acc]);
-                }
+                    mbar_arrive(&sh.tempty[acc]);
             }
         }
     }
@@ -403,31 +470,100 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
         __syncthreads();
     }
-    if constexpr (kCluster) cluster_sync();
-    if constexpr (SPLIT) {
-        // every CTA of the cluster adds up its share of the columns, slice 0 first
-        if (warp >= 4 && !*abort_flag) {
-            const Tile tile = decode_tile(p, unit);
-            const int width = BN / p.split, e = tid - 128;
-            for (int i = e; i < width / 8 * 128; i += kEpiWarps * 32) {
-                const int r = i & 127, c = (int)rank * width + (i >> 7) * 8;
-                float v[8] = {};
-                for (int s = 0; s < p.split; ++s) {
-                    const uint32_t from = map_rank(base + (uint32_t)(c * 128 + r) * 4, s);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] += ld_cluster(from + j * 512);
-                }
-                epi.apply8(tile.batch, tile.tm * 128 + r, tile.tn * BN + c, v, p.sym && tile.tm != tile.tn);
-            }
-        }
-        __syncwarp();
-        cluster_sync();
-    }
+    if constexpr (CG == 2) cluster_sync();
     tc_fence_after();
     if (warp == 2) tmem_dealloc_cg<CG>(tmem, 2 * BN);
 }
 
+// ---- slices of K ---------------------------------------------------------------
+
+// The sums of one slice, fp32, in the workspace: [slice][batch][rows][pitch].
+struct SliceEpi {
+    static constexpr bool kWholeRow = false, kMirror = false, kScalar = false;
+    float* out;
+    int rows, pitch;
+    template <int R> struct Ops {};
+    template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
+    template <int R>
+    __device__ __forceinline__ void apply(const Ops<R>&, int batch, int row, int step, int col, float (&v)[R][8]) const {
+        if (col >= pitch) return;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (row + i * step >= rows) return;
+            float4* q = reinterpret_cast<float4*>(out + ((long long)batch * rows + row + i * step) * pitch + col);
+            q[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+            q[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+        }
+    }
+};
+
+struct SliceSums {
+    const float* in;
+    int rows, pitch, slices, batch;
+    int sym;                // tile edge of a symmetric result, else 0: patches left of the diagonal tiles were not computed
+};
+
+// Adds the slices, first to last, and applies the epilogue. A warp per 32 x 32 patch, grid (patches / 8, 1, batch).
+template <class Epi>
+__global__ void __launch_bounds__(256) join_slices_kernel(const __grid_constant__ SliceSums p, const __grid_constant__ Epi epi) {
+    __shared__ __align__(16) float patches[Epi::kMirror || Epi::kScalar ? kEpiWarps * 32 * kPatchPitch : 4];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, across = (p.pitch + 31) / 32;
+    const long long patch = (long long)blockIdx.x * 8 + warp;
+    const int row = (int)(patch / across) * 32, col = (int)(patch % across) * 32, batch = blockIdx.z;
+    if (row >= p.rows || (p.sym && col / p.sym < row / p.sym)) return;
+    const int r = row + (lane >> 2), c = col + (lane & 3) * 8;
+    typename Epi::template Ops<4> ops;
+    epi.load(ops, batch, r, 8, c);
+    float v[4][8] = {};
+    if (c < p.pitch) {
+        const long long stride = (long long)p.batch * p.rows * p.pitch;
+        const float* from = p.in + ((long long)batch * p.rows + r) * p.pitch + c;
+#pragma unroll 2
+        for (int s = 0; s < p.slices; ++s, from += stride) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (r + i * 8 >= p.rows) continue;
+                const float4 a = *reinterpret_cast<const float4*>(from + (long long)i * 8 * p.pitch);
+                const float4 b = *reinterpret_cast<const float4*>(from + (long long)i * 8 * p.pitch + 4);
+                v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
+                v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
+            }
+        }
+    }
+    epi.apply(ops, batch, r, 8, c, v);
+    if constexpr (Epi::kMirror) {
+        if (p.sym && col / p.sym != row / p.sym)
+            store_mirror_patch(epi, patches + warp * 32 * kPatchPitch, lane, batch, row, col, v);
+    }
+    if constexpr (Epi::kScalar) {
+        if (epi.scalar()) store_scalar_patch(epi, patches + warp * 32 * kPatchPitch, lane, batch, row, col, v);
+    }
+}
+
 // ---- host side ------------------------------------------------------------------
+
+// A product [m x n x k] of `batch` matrices, and how it is run.
+struct Problem {
+    int m, n;
+    long long k;
+    int batch;
+    bool bf16;
+    bool sym;               // A A^T: half of the tiles suffices
+};
+struct Shape {
+    bool pairs;
+    int slices;
+    bool half;              // compute the tiles on and above the diagonal only and mirror them
+};
+// The shape with the least expected time. whole_row: the epilogue cannot take slices. Slices need slice_bytes of scratch.
+Shape shape(const Problem& q, bool whole_row, size_t scratch_bytes);
+size_t slice_bytes(const Problem& q, int slices);
+inline size_t scratch_bytes(const Problem& q) {      // what shape() would like to have
+    const int s = shape(q, false, ~(size_t)0).slices;
+    return s > 1 ? slice_bytes(q, s) : 0;
+}
 
 // One operand: `rows` rows of `inner` 16-bit elements, `pitch` elements apart, `batch` matrices `stride` elements
 // apart. mn: the inner direction is the result's (M or N) and the rows are K.
@@ -440,63 +576,71 @@ struct Operand {
 };
 
 ac_status make_map(CUtensorMap* map, const Operand& o, bool bf16, int tile_rows);     // mm_host.cu
-// Tile grid, raster and instruction descriptor of a product [m x n x k].
-Params make_params(int m, int n, long long k, int batch, int cg, int bn, bool a_mn, bool b_mn, bool bf16, bool sym);
-// Whether 256 x 256 tiles of CTA pairs fill the GPU; else 128 x 128 tiles and, in *split, the CTAs that share one.
-bool use_pairs(int m, int n, long long k, int batch, bool sym, int* split);
+// Tile grid, raster and instruction descriptor.
+Params make_params(const Problem& q, const Shape& s, bool a_mn, bool b_mn);
 
-template <int CG, int BN, bool AMN, bool BMN, bool SPLIT, class Epi>
-ac_status launch_one(const Operand& a, const Operand& b, bool bf16, const Params& p, const Epi& epi, cudaStream_t st) {
+struct Call {               // what the launches of one call share
+    uint32_t* status;
+    bool reset;             // the next launch resets the status block
+    void* scratch;          // for slices
+    size_t scratch_bytes;
+    cudaStream_t stream;
+};
+
+template <int CG, int BN, bool AMN, bool BMN, class Epi>
+ac_status launch_one(const Operand& a, const Operand& b, const Problem& q, const Shape& s, Call& call, const Epi& epi) {
     static bool attr_done[64] = {};
+    Params p = make_params(q, s, AMN, BMN);
+    p.status = call.status;
+    p.reset_status = call.reset;
+    call.reset = false;
     CUtensorMap ta, tb;
-    ac_status rc = make_map(&ta, a, bf16, 128);
-    if (rc == AC_OK) rc = make_map(&tb, b, bf16, BN / CG);
-    auto kernel = mm_kernel<CG, BN, AMN, BMN, SPLIT, Epi>;
-    if (rc == AC_OK) rc = ensure_smem_limit(kernel, smem_bytes<CG, BN>(), attr_done);
+    ac_status rc = make_map(&ta, a, q.bf16, 128);
+    if (rc == AC_OK) rc = make_map(&tb, b, q.bf16, BN / CG);
+    auto kernel = mm_kernel<CG, BN, AMN, BMN, Epi>;
+    if (rc == AC_OK) rc = ensure_smem_limit(kernel, smem_bytes<CG, BN, Epi>(), attr_done);
     if (rc != AC_OK) return rc;
-    const int per_tile = SPLIT ? p.split : CG;
-    const int units = SPLIT ? p.tiles : (p.tiles < kNumSMs / CG ? p.tiles : kNumSMs / CG);
+    const int units = p.tiles < kNumSMs / CG ? p.tiles : kNumSMs / CG;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(units * per_tile);
+    cfg.gridDim = dim3(units * CG);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem_bytes<CG, BN>();
-    cfg.stream = st;
+    cfg.dynamicSmemBytes = smem_bytes<CG, BN, Epi>();
+    cfg.stream = call.stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = per_tile;
+    attr[1].val.clusterDim.x = CG;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = per_tile > 1 ? 2 : 1;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
     AC_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, ta, tb, p, epi));
     return AC_OK;
 }
 
-// D = A B^T for operands of one layout pair, on tiles of CTA pairs or on 128 x 128 tiles whose K `split` CTAs share.
 template <bool AMN, bool BMN, class Epi>
-ac_status launch_shaped(bool pairs, int split, const Operand& a, const Operand& b, int m, int n, long long k, int batch,
-                        bool bf16, bool sym, uint32_t* status, bool reset, const Epi& epi, cudaStream_t st) {
-    Params p = make_params(m, n, k, batch, pairs ? 2 : 1, pairs ? 256 : 128, AMN, BMN, bf16, sym);
-    p.status = status;
-    p.reset_status = reset;
-    if (pairs) return launch_one<2, 256, AMN, BMN, false>(a, b, bf16, p, epi, st);
-    if constexpr (!Epi::kWholeRow) {
-        if (split > 1) {
-            p.split = split;
-            return launch_one<1, 128, AMN, BMN, true>(a, b, bf16, p, epi, st);
-        }
-    }
-    return launch_one<1, 128, AMN, BMN, false>(a, b, bf16, p, epi, st);
+ac_status launch_shaped(const Operand& a, const Operand& b, const Problem& q, const Shape& s, Call& call, const Epi& epi) {
+    return s.pairs ? launch_one<2, 256, AMN, BMN>(a, b, q, s, call, epi) : launch_one<1, 128, AMN, BMN>(a, b, q, s, call, epi);
 }
 
-// The same with the shape chosen by use_pairs.
+// D = A B^T for operands of one layout pair.
 template <bool AMN, bool BMN, class Epi>
-ac_status launch(const Operand& a, const Operand& b, int m, int n, long long k, int batch, bool bf16, bool sym,
-                 uint32_t* status, bool reset, const Epi& epi, cudaStream_t st) {
-    int split = 1;
-    const bool pairs = use_pairs(m, n, k, batch, sym, &split);
-    return launch_shaped<AMN, BMN>(pairs, split, a, b, m, n, k, batch, bf16, sym, status, reset, epi, st);
+ac_status launch(const Operand& a, const Operand& b, const Problem& q, Call& call, const Epi& epi) {
+    const Shape s = shape(q, Epi::kWholeRow, call.scratch_bytes);
+    if constexpr (!Epi::kWholeRow) {
+        if (s.slices > 1) {
+            const int pitch = (q.n + 7) / 8 * 8;
+            const SliceEpi slice{static_cast<float*>(call.scratch), q.m, pitch};
+            const ac_status rc = launch_shaped<AMN, BMN>(a, b, q, s, call, slice);
+            if (rc != AC_OK) return rc;
+            const SliceSums sums{slice.out, q.m, pitch, s.slices, q.batch, s.half ? (s.pairs ? 256 : 128) : 0};
+            const long long patches = (long long)((q.m + 31) / 32) * ((pitch + 31) / 32);
+            AC_CUDA_TRY(launch_after(join_slices_kernel<Epi>, dim3((unsigned)((patches + 7) / 8), 1, q.batch), dim3(256), 0,
+                                     call.stream, sums, epi));
+            return AC_OK;
+        }
+    }
+    return launch_shaped<AMN, BMN>(a, b, q, s, call, epi);
 }
 
 }  // namespace mm

@@ -41,42 +41,64 @@ ac_status make_map(CUtensorMap* map, const Operand& o, bool bf16, int tile_rows)
     return AC_OK;
 }
 
-Params make_params(int m, int n, long long k, int batch, int cg, int bn, bool a_mn, bool b_mn, bool bf16, bool sym) {
+Params make_params(const Problem& q, const Shape& s, bool a_mn, bool b_mn) {
     Params p{};
-    p.m = m;
-    p.n = n;
-    p.ktiles = ceil_div(k, kBK);
-    p.tiles_m = ceil_div(m, 128 * cg);
-    p.tiles_n = ceil_div(n, bn);
-    p.sym = sym;
-    p.per_batch = sym ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
-    p.tiles = p.per_batch * batch;
+    const int cg = s.pairs ? 2 : 1, edge = 128 * cg;      // tiles are square
+    p.m = q.m;
+    p.n = q.n;
+    p.ktiles = ceil_div(q.k, kBK);
+    p.tiles_m = ceil_div(q.m, edge);
+    p.tiles_n = ceil_div(q.n, edge);
+    p.half = s.half;
+    p.same = q.sym;
+    p.batch = q.batch;
+    p.slices = s.slices;
+    p.per_batch = s.half ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
+    p.tiles = p.per_batch * q.batch * s.slices;
     // The smaller operand is cycled through while the larger one streams past once, as far as the panels of the
     // smaller one fit a third of the L2 (126 MB); at least 8 tiles, so that the tiles in flight stay squarish.
-    p.fast_m = m <= n;
-    const long long panel = (p.fast_m ? 128ll * cg : bn) * k * 2;
-    long long g = (40ll << 20) / panel;
+    p.fast_m = q.m <= q.n;
+    const long long panel = edge * q.k * 2 / s.slices;
+    const long long g = (40ll << 20) / (panel > 0 ? panel : 1);
     const int tf = p.fast_m ? p.tiles_m : p.tiles_n;
-    p.group = (int)(g < 8 ? 8 : g);
+    p.group = (int)(g < 8 ? 8 : g < tf ? g : tf);
     if (p.group > tf) p.group = tf;
-    p.split = 1;
-    const uint32_t type = bf16 ? 1u : 0u;
+    const uint32_t type = q.bf16 ? 1u : 0u;
     p.idesc = (1u << 4) | (type << 7) | (type << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-              ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(128 * cg >> 4) << 24);
+              ((uint32_t)(edge >> 3) << 17) | ((uint32_t)(edge >> 4) << 24);
     return p;
 }
 
-bool use_pairs(int m, int n, long long k, int batch, bool sym, int* split) {
-    const int tm = ceil_div(m, 256), tn = ceil_div(n, 256);
-    const long long large = (long long)(sym ? tn * (tn + 1) / 2 : tm * tn) * batch;
-    *split = 1;
-    if (large >= kNumSMs / 2) return true;
-    const int sm = ceil_div(m, 128), sn = ceil_div(n, 128);
-    const long long small = (long long)(sym ? sn * (sn + 1) / 2 : sm * sn) * batch;
-    const int ktiles = ceil_div(k, kBK);
-    // as many slices as leave every SM at most one CTA, each at least two K-tiles long
-    while (*split < kMaxSplit && small * *split * 2 <= kNumSMs && ktiles >= *split * 4) *split *= 2;
-    return false;
+size_t slice_bytes(const Problem& q, int slices) {
+    return (size_t)slices * q.batch * q.m * ((q.n + 7) / 8 * 8) * 4;
+}
+
+// Expected time in us, from measured rates: a K-tile takes an SM 0.27 us in either shape; the epilogue of a tile 2 us of
+// a lone CTA and 4 us of a pair, twice that where it is mirrored, hidden behind the next tile's products where there is
+// one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s).
+Shape shape(const Problem& q, bool whole_row, size_t scratch) {
+    Shape best{false, 1, false};
+    double least = 1e30;
+    const int ktiles = ceil_div(q.k, kBK);
+    for (int pairs = 0; pairs < 2; ++pairs) {
+        const int edge = pairs ? 256 : 128, units = pairs ? kNumSMs / 2 : kNumSMs;
+        const long long tm = ceil_div(q.m, edge), tn = ceil_div(q.n, edge);
+        for (int half = 0; half <= (q.sym ? 1 : 0); ++half) {
+            const long long tiles = (half ? tn * (tn + 1) / 2 : tm * tn) * q.batch;
+            const double tail = (pairs ? 4.0 : 2.0) * (half ? 2 : 1);
+            for (int s = 1; s <= (whole_row ? 1 : kMaxSlices) && (s == 1 || s * 2 <= ktiles); ++s) {
+                if (s > 1 && slice_bytes(q, s) > scratch) break;
+                const double waves = (double)((tiles * s + units - 1) / units), main = (double)ktiles / s * 0.27;
+                double t = waves * (main > tail ? main : tail) + (main > tail ? tail : main);
+                if (s > 1) t += 6.0 + (double)slice_bytes(q, s) * 2 / 5e6;
+                if (t < least * 0.97) {      // the simpler one unless the other is worth it
+                    least = t;
+                    best = Shape{pairs != 0, s, half != 0};
+                }
+            }
+        }
+    }
+    return best;
 }
 
 }  // namespace mm

@@ -28,7 +28,7 @@ constexpr int kNormBlocks = 512;     // partial sums of squares per matrix at mo
 // with D the diagonal, A^2 = O^2 + D O + O D + D^2. The diagonals go to fp32 vectors, zeros take their place in the fp16
 // matrices.
 struct SymEpi {
-    static constexpr bool kWholeRow = false;
+    static constexpr bool kWholeRow = false, kMirror = true, kScalar = false;
     const __half* a;      // null: A from the accumulators
     const float* da;
     __half* out;
@@ -36,31 +36,55 @@ struct SymEpi {
     float b, c;
     int n;
     long long pitch;
-    __device__ __forceinline__ void apply8(int batch, int row, int col, float (&v)[8], bool mirror) const {
-        if (row >= n || col >= n) return;
-        const long long base = (long long)batch * n * pitch, at = base + row * pitch + col, line = batch * pitch;
-        if (a) {
-            float x[8];
-            load8(a + at, x);
-            const float d = da[line + row];
-            const float4 e = *reinterpret_cast<const float4*>(da + line + col), f = *reinterpret_cast<const float4*>(da + line + col + 4);
-            const float other[8] = {e.x, e.y, e.z, e.w, f.x, f.y, f.z, f.w};
+    template <int R> struct Ops {
+        uint4 x[R];
+        float d[R];
+        float4 e, f;
+    };
+    template <int R>
+    __device__ __forceinline__ void load(Ops<R>& o, int batch, int row, int step, int col) const {
+        if (!a || col >= n) return;
+        const long long base = (long long)batch * n * pitch + col, line = batch * pitch;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                v[j] = row == col + j ? fmaf(b, d, c * fmaf(d, d, v[j])) : fmaf(b, x[j], c * fmaf(d + other[j], x[j], v[j]));
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (row == col + j) {
-                dout[line + row] = v[j];
-                v[j] = 0.f;
+        for (int i = 0; i < R; ++i)
+            if (row + i * step < n) {
+                o.x[i] = *reinterpret_cast<const uint4*>(a + base + (row + i * step) * pitch);
+                o.d[i] = da[line + row + i * step];
             }
-        store8(out + at, v);
-        if (mirror) {
+        o.e = *reinterpret_cast<const float4*>(da + line + col);
+        o.f = *reinterpret_cast<const float4*>(da + line + col + 4);
+    }
+    template <int R>
+    __device__ __forceinline__ void apply(const Ops<R>& o, int batch, int row, int step, int col, float (&v)[R][8]) const {
+        if (col >= n) return;
+        const long long base = (long long)batch * n * pitch + col, line = batch * pitch;
+        if (a) {
+            const float other[8] = {o.e.x, o.e.y, o.e.z, o.e.w, o.f.x, o.f.y, o.f.z, o.f.w};
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float y[8];
+                unpack8(o.x[i], y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    v[i][j] = row + i * step == col + j ? fmaf(b, o.d[i], c * fmaf(o.d[i], o.d[i], v[i][j]))
+                                                        : fmaf(b, y[j], c * fmaf(o.d[i] + other[j], y[j], v[i][j]));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int r = row + i * step;
+            if (r >= n) return;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (col + j < n) out[base + (long long)(col + j) * pitch + row] = __float2half(v[j]);
+                if (r == col + j) {
+                    dout[line + r] = v[i][j];
+                    v[i][j] = 0.f;
+                }
+            store8(out + base + r * pitch, v[i]);
         }
+    }
+    __device__ __forceinline__ void store_mirror(int batch, int row, int col, const float (&v)[8]) const {
+        if (row < n && col < n) store8(out + ((long long)batch * n + row) * pitch + col, v);
     }
 };
 
@@ -68,7 +92,7 @@ struct SymEpi {
 // the hi term alone while steps remain that would amplify the difference, all of X in the last two.
 template <bool TALL>
 struct StepEpi {
-    static constexpr bool kWholeRow = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kScalar = true;
     const __half* hi;
     __half* lo;             // read and written by the same thread
     __half* hi_out;
@@ -77,38 +101,59 @@ struct StepEpi {
     float a, scale, lo_share;
     int rows, cols;
     long long pitch, sym_pitch;
-    __device__ __forceinline__ void apply8(int batch, int row, int col, float (&v)[8], bool) const {
-        if (row >= rows || col >= cols) return;
-        const long long at = ((long long)batch * rows + row) * pitch + col;
+    __device__ __forceinline__ bool scalar() const { return update && cols % 8 != 0; }
+    __device__ __forceinline__ void store1(int batch, int row, int col, float v) const {
+        if (row < rows && col < cols) update[((long long)batch * rows + row) * cols + col] = __float2bfloat16(v);
+    }
+    template <int R> struct Ops {
+        uint4 x[R], y[R];
+        float f[R];
+        float4 e, g;
+    };
+    template <int R>
+    __device__ __forceinline__ void load(Ops<R>& o, int batch, int row, int step, int col) const {
+        if (col >= cols) return;
+        const long long base = (long long)batch * rows;
         const float* d = dp + batch * sym_pitch;
-        float x[8], y[8], f[8];
-        load8(hi + at, x);
-        load8(lo + at, y);
-        if constexpr (TALL) {
-            const float4 e = *reinterpret_cast<const float4*>(d + col), g = *reinterpret_cast<const float4*>(d + col + 4);
-            f[0] = e.x; f[1] = e.y; f[2] = e.z; f[3] = e.w;
-            f[4] = g.x; f[5] = g.y; f[6] = g.z; f[7] = g.w;
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = d[row];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = fmaf(a, x[j] + y[j], fmaf(f[j], fmaf(lo_share, y[j], x[j]), v[j]));
-        if (update) {
-            const long long to = ((long long)batch * rows + row) * cols + col;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= scale;
-            if (cols % 8 == 0) {
-                store8(update + to, v);
-            } else {
-                for (int j = 0; j < 8 && col + j < cols; ++j) update[to + j] = __float2bfloat16(v[j]);
+        for (int i = 0; i < R; ++i)
+            if (row + i * step < rows) {
+                o.x[i] = *reinterpret_cast<const uint4*>(hi + (base + row + i * step) * pitch + col);
+                o.y[i] = *reinterpret_cast<const uint4*>(lo + (base + row + i * step) * pitch + col);
+                if constexpr (!TALL) o.f[i] = d[row + i * step];
             }
-            return;
+        if constexpr (TALL) {
+            o.e = *reinterpret_cast<const float4*>(d + col);
+            o.g = *reinterpret_cast<const float4*>(d + col + 4);
         }
-        store8(hi_out + at, v);
+    }
+    template <int R>
+    __device__ __forceinline__ void apply(const Ops<R>& o, int batch, int row, int step, int col, float (&v)[R][8]) const {
+        if (col >= cols) return;
+        const long long base = (long long)batch * rows;
+        const float f[8] = {o.e.x, o.e.y, o.e.z, o.e.w, o.g.x, o.g.y, o.g.z, o.g.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] -= __half2float(__float2half(v[j]));
-        store8(lo + at, v);
+        for (int i = 0; i < R; ++i) {
+            const int r = row + i * step;
+            if (r >= rows) return;
+            float h[8], l[8];
+            unpack8(o.x[i], h);
+            unpack8(o.y[i], l);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[i][j] = fmaf(a, h[j] + l[j], fmaf(TALL ? f[j] : o.f[i], fmaf(lo_share, l[j], h[j]), v[i][j]));
+            if (update) {
+                const long long to = (base + r) * cols + col;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] *= scale;
+                if (cols % 8 == 0) store8(update + to, v[i]);
+                continue;
+            }
+            store8(hi_out + (base + r) * pitch + col, v[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] -= __half2float(__float2half(v[i][j]));
+            store8(lo + (base + r) * pitch + col, v[i]);
+        }
     }
 };
 
@@ -260,7 +305,7 @@ struct MuonPlan {
     int k;                  // min(rows, cols)
     long long pitch, sym_pitch;
     int blocks;
-    size_t off_partial, off_hi[2], off_lo, off_a, off_p, off_da, off_dp, bytes;
+    size_t off_partial, off_hi[2], off_lo, off_a, off_p, off_da, off_dp, off_slices, slice_bytes, bytes;
 };
 
 bool valid(const ac_muon_desc* d) {
@@ -272,6 +317,18 @@ bool valid(const ac_muon_desc* d) {
         if (!(x - x == 0.f)) return false;      // infinite or NaN
     if (d->eps < 0.f) return false;
     return (long long)d->rows * d->cols < (1ll << 36) / d->batch;
+}
+
+Problem gram_problem(const ac_muon_desc& d) {
+    const int k = d.rows < d.cols ? d.rows : d.cols;
+    return Problem{k, k, d.rows < d.cols ? d.cols : d.rows, d.batch, false, true};
+}
+Problem square_problem(const ac_muon_desc& d) {
+    const int k = d.rows < d.cols ? d.rows : d.cols;
+    return Problem{k, k, k, d.batch, false, true};
+}
+Problem step_problem(const ac_muon_desc& d) {
+    return Problem{d.rows, d.cols, d.rows < d.cols ? d.rows : d.cols, d.batch, false, false};
 }
 
 MuonPlan plan_muon(const ac_muon_desc& d) {
@@ -297,6 +354,12 @@ MuonPlan plan_muon(const ac_muon_desc& d) {
     p.off_p = take(s);
     p.off_da = take((long long)d.batch * p.sym_pitch * 4);
     p.off_dp = take((long long)d.batch * p.sym_pitch * 4);
+    const Problem all[] = {gram_problem(d), square_problem(d), step_problem(d)};
+    for (const Problem& q : all) {
+        const size_t b = scratch_bytes(q);
+        if (b > p.slice_bytes) p.slice_bytes = b;
+    }
+    p.off_slices = take((long long)p.slice_bytes);
     p.bytes = at;
     return p;
 }
@@ -326,15 +389,16 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
         return AC_OK;
     }
     const bool tall = d.rows > d.cols;
+    Call call{status, false, ws + p.off_slices, p.slice_bytes, st};
+    const Problem qa = gram_problem(d), qp = square_problem(d), qx = step_problem(d);
     const long long x_stride = (long long)d.rows * p.pitch, s_stride = (long long)p.k * p.sym_pitch;
     for (int i = 0; i < d.steps; ++i) {
         const __half* X = hi[i & 1];
         const Operand Xk{X, d.cols, d.rows, p.pitch, d.batch, x_stride, false}, Xt{X, d.cols, d.rows, p.pitch, d.batch, x_stride, true};
         const Operand Ak{A, p.k, p.k, p.sym_pitch, d.batch, s_stride, false}, Pk{P, p.k, p.k, p.sym_pitch, d.batch, s_stride, false};
         const SymEpi gram{nullptr, nullptr, A, dA, 0.f, 0.f, p.k, p.sym_pitch}, poly{A, dA, P, dP, d.b, d.c, p.k, p.sym_pitch};
-        ac_status rc = tall ? launch<true, true>(Xt, Xt, p.k, p.k, d.rows, d.batch, false, true, status, false, gram, st)
-                            : launch<false, false>(Xk, Xk, p.k, p.k, d.cols, d.batch, false, true, status, false, gram, st);
-        if (rc == AC_OK) rc = launch<false, false>(Ak, Ak, p.k, p.k, p.k, d.batch, false, true, status, false, poly, st);
+        ac_status rc = tall ? launch<true, true>(Xt, Xt, qa, call, gram) : launch<false, false>(Xk, Xk, qa, call, gram);
+        if (rc == AC_OK) rc = launch<false, false>(Ak, Ak, qp, call, poly);
         auto step = [&](auto& e, auto&& go) {
             e.hi = X;
             e.lo = lo;
@@ -352,10 +416,10 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
         };
         if (rc == AC_OK && tall) {
             StepEpi<true> e;
-            rc = step(e, [&](auto& f) { return launch<false, false>(Xk, Pk, d.rows, d.cols, p.k, d.batch, false, false, status, false, f, st); });
+            rc = step(e, [&](auto& f) { return launch<false, false>(Xk, Pk, qx, call, f); });
         } else if (rc == AC_OK) {
             StepEpi<false> e;
-            rc = step(e, [&](auto& f) { return launch<false, true>(Pk, Xt, d.rows, d.cols, p.k, d.batch, false, false, status, false, f, st); });
+            rc = step(e, [&](auto& f) { return launch<false, true>(Pk, Xt, qx, call, f); });
         }
         if (rc != AC_OK) return rc;
     }
