@@ -61,7 +61,7 @@ __device__ __forceinline__ void logits32(const Ce& c, uint32_t taddr, int col, f
 // Statistics of a row's 128 columns; KEEP: and exp(l - m) as fp16.
 template <bool KEEP>
 struct StatsEpi : Ce {
-    static constexpr bool kWholeRow = true, kMirror = false;
+    static constexpr bool kWholeRow = true;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
@@ -114,7 +114,7 @@ struct StatsEpi : Ce {
 
 // g of a piece from its logits and the rows' lse.
 struct GradEpi : Ce {
-    static constexpr bool kWholeRow = true, kMirror = false;
+    static constexpr bool kWholeRow = true;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>

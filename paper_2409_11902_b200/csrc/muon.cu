@@ -14,7 +14,7 @@
 // hi alone gives 2e-2 and bf16 1e-1. The diagonals of A and P = b A + c A^2, their largest entries, are carried apart in fp32.
 // A and P are symmetric: half of their tiles are computed and written
 // twice.
-#include "mm_core.cuh"
+#include "muon_onchip.cuh"
 
 namespace ac {
 
@@ -302,6 +302,7 @@ __global__ void __launch_bounds__(256) unstepped_kernel(const __grid_constant__ 
 inline long long up(long long a, long long b) { return (a + b - 1) / b * b; }
 
 struct MuonPlan {
+    int ctas, slabs;        // on-chip kernel: CTAs per matrix (0: the kernels for large matrices), slabs of 64 columns per CTA
     int k;                  // min(rows, cols)
     long long pitch, sym_pitch;
     int blocks;
@@ -334,6 +335,19 @@ Problem step_problem(const ac_muon_desc& d) {
 MuonPlan plan_muon(const ac_muon_desc& d) {
     MuonPlan p{};
     p.k = d.rows < d.cols ? d.rows : d.cols;
+    const int l = d.rows < d.cols ? d.cols : d.rows, all = (l + 63) / 64;
+    if (p.k <= kOnchipK && l <= kOnchipL) {
+        // The fewest slabs per CTA that 8 CTAs, and a GPU's share per matrix, allow
+        const int most = kNumSMs / d.batch < 1 ? 1 : kNumSMs / d.batch < kOnchipCluster ? kNumSMs / d.batch : kOnchipCluster;
+        p.slabs = (all + most - 1) / most;
+        if (p.slabs > kOnchipSlabs) p.slabs = kOnchipSlabs;
+        p.ctas = (all + p.slabs - 1) / p.slabs;
+        const long long k16 = up(p.k, 16);
+        p.off_partial = kStatusBlockBytes;
+        p.off_hi[0] = p.off_partial + (size_t)up((long long)d.batch * p.ctas * 4, 256);
+        p.bytes = p.off_hi[0] + (size_t)(2 * d.batch * p.ctas * k16 * 128 * 4);
+        return p;
+    }
     p.pitch = up(d.cols, 8);
     p.sym_pitch = up(p.k, 8);
     const long long n = (long long)d.rows * d.cols;
@@ -354,8 +368,8 @@ MuonPlan plan_muon(const ac_muon_desc& d) {
     p.off_p = take(s);
     p.off_da = take((long long)d.batch * p.sym_pitch * 4);
     p.off_dp = take((long long)d.batch * p.sym_pitch * 4);
-    const Problem all[] = {gram_problem(d), square_problem(d), step_problem(d)};
-    for (const Problem& q : all) {
+    const Problem products[] = {gram_problem(d), square_problem(d), step_problem(d)};
+    for (const Problem& q : products) {
         const size_t b = scratch_bytes(q);
         if (b > p.slice_bytes) p.slice_bytes = b;
     }
@@ -369,6 +383,29 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
     const MuonPlan p = plan_muon(d);
     char* ws = static_cast<char*>(workspace);
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
+    if (p.ctas) {
+        static bool attr_done[64] = {};
+        const ac_status rc = ensure_smem_limit(onchip_kernel, (int)kOnchipSmem, attr_done);
+        if (rc != AC_OK) return rc;
+        const Onchip o{grad, v_in, v_out, static_cast<__nv_bfloat16*>(update), reinterpret_cast<float*>(ws + p.off_hi[0]),
+                       reinterpret_cast<float*>(ws + p.off_partial), status, d.momentum, d.a, d.b, d.c, d.eps, d.scale,
+                       d.nesterov, d.dtype == AC_BF16, d.steps, d.rows, d.cols, p.k, d.rows < d.cols ? d.cols : d.rows, p.slabs};
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(p.ctas, d.batch);
+        cfg.blockDim = dim3(256);
+        cfg.dynamicSmemBytes = kOnchipSmem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = p.ctas;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        AC_CUDA_TRY(cudaLaunchKernelEx(&cfg, onchip_kernel, o));
+        return AC_OK;
+    }
     __half* hi[2] = {reinterpret_cast<__half*>(ws + p.off_hi[0]), reinterpret_cast<__half*>(ws + p.off_hi[1])};
     __half* lo = reinterpret_cast<__half*>(ws + p.off_lo);
     __half *A = reinterpret_cast<__half*>(ws + p.off_a), *P = reinterpret_cast<__half*>(ws + p.off_p);
