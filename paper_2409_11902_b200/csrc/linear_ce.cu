@@ -47,9 +47,12 @@ __device__ __forceinline__ void logits32(const Ce& c, uint32_t taddr, int col, f
 #pragma unroll
     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
     if (c.bias) {
+        const __nv_bfloat16* b = c.bias + c.first;       // clamped, not guarded: guarded loads would wait for one another
+        float add[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (col + j < c.width) x[j] += __bfloat162float(c.bias[c.first + col + j]);
+        for (int j = 0; j < 32; ++j) add[j] = __bfloat162float(b[min(col + j, c.width - 1)]);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] += add[j];
     }
     if (col + 32 > c.width) {
 #pragma unroll

@@ -22,7 +22,7 @@ using namespace mm;
 
 namespace {
 
-constexpr int kNormBlocks = 512;     // partial sums of squares per matrix at most
+constexpr int kNormBlocks = 2368;    // 16 blocks per SM; each leaves a partial sum of squares
 
 // Square symmetric results. A = X X^T, or P = b A + c A^2 from the accumulated square of A's off-diagonal part O:
 // with D the diagonal, A^2 = O^2 + D O + O D + D^2. The diagonals go to fp32 vectors, zeros take their place in the fp16
@@ -171,28 +171,6 @@ struct Elements {
 };
 
 template <int W>
-__device__ __forceinline__ void load_grad(const Elements& e, long long at, float* g) {
-    if (e.bf16) {
-        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(e.grad) + at;
-        if constexpr (W == 4) {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
-            const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
-            const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
-            g[0] = a.x; g[1] = a.y; g[2] = b.x; g[3] = b.y;
-        } else {
-            g[0] = __bfloat162float(*p);
-        }
-    } else {
-        const float* p = static_cast<const float*>(e.grad) + at;
-        if constexpr (W == 4) {
-            const float4 u = *reinterpret_cast<const float4*>(p);
-            g[0] = u.x; g[1] = u.y; g[2] = u.z; g[3] = u.w;
-        } else {
-            g[0] = *p;
-        }
-    }
-}
-template <int W>
 __device__ __forceinline__ void load_f32(const float* p, float* v) {
     if constexpr (W == 4) {
         const float4 u = *reinterpret_cast<const float4*>(p);
@@ -202,33 +180,49 @@ __device__ __forceinline__ void load_f32(const float* p, float* v) {
     }
 }
 
-// v' and the block's share of |u|^2. W: elements per access, 4 where rows of the flat array allow it.
+// u and, where `write`, v' of W elements.
+template <int W>
+__device__ __forceinline__ void form_u(const Elements& e, long long at, bool write, float (&g)[W], const float (&v)[W]) {
+    if (!e.v_in) return;
+    float w[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        w[j] = write ? e.beta * v[j] + g[j] : v[j];
+        g[j] = e.nesterov ? fmaf(e.beta, w[j], g[j]) : w[j];
+    }
+    if (!write) return;
+    if constexpr (W == 4)
+        *reinterpret_cast<float4*>(e.v_out + at) = make_float4(w[0], w[1], w[2], w[3]);
+    else
+        e.v_out[at] = w[0];
+}
+
+constexpr int kAhead = 4;       // accesses of a thread in flight
+
+// v' and the block's share of |u|^2. W: elements per access, 4 where no access crosses a row.
 template <int W>
 __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ Elements e) {
     __shared__ float part[8];
     pdl_launch_dependents();
     pdl_wait();
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) { e.status[0] = 0u; e.status[1] = 0u; }
-    const long long n = (long long)e.rows * e.cols, base = n * blockIdx.y;
+    const long long n = (long long)e.rows * e.cols, base = n * blockIdx.y, step = (long long)gridDim.x * 256 * W;
     float sum = 0.f;
-    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * W; i < n; i += (long long)gridDim.x * 256 * W) {
-        float g[W];
-        load_grad<W>(e, base + i, g);
-        if (e.v_in) {
-            float v[W];
-            load_f32<W>(e.v_in + base + i, v);
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * W; i < n; i += step * kAhead) {
+        float g[kAhead][W], v[kAhead][W];
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                v[j] = e.beta * v[j] + g[j];
-                g[j] = e.nesterov ? fmaf(e.beta, v[j], g[j]) : v[j];
+        for (int q = 0; q < kAhead; ++q)
+            if (i + q * step < n) {
+                load_grad<W>(e.grad, e.bf16, base + i + q * step, g[q]);
+                if (e.v_in) load_f32<W>(e.v_in + base + i + q * step, v[q]);
             }
-            if constexpr (W == 4)
-                *reinterpret_cast<float4*>(e.v_out + base + i) = make_float4(v[0], v[1], v[2], v[3]);
-            else
-                e.v_out[base + i] = v[0];
-        }
 #pragma unroll
-        for (int j = 0; j < W; ++j) sum = fmaf(g[j], g[j], sum);
+        for (int q = 0; q < kAhead; ++q)
+            if (i + q * step < n) {
+                form_u<W>(e, base + i + q * step, true, g[q], v[q]);
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum = fmaf(g[q][j], g[q][j], sum);
+            }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -240,7 +234,7 @@ __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ E
     }
 }
 
-// X = u / (|u| + eps) as hi + lo. Grid (norm blocks, batch): as many blocks as partial sums.
+// X = u / (|u| + eps) as hi + lo. As many blocks as partial sums.
 template <int W>
 __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ Elements e) {
     __shared__ float part[8];
@@ -255,34 +249,35 @@ __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ 
     sum = 0.f;
     for (int w = 0; w < 8; ++w) sum += part[w];
     const float inv = 1.f / (sqrtf(sum) + e.eps);
-    const long long n = (long long)e.rows * e.cols, base = n * blockIdx.y;
-    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * W; i < n; i += (long long)gridDim.x * 256 * W) {
-        float g[W];
-        if (e.v_in) {
-            float v[W];
-            load_f32<W>(e.v_out + base + i, v);
-            if (e.nesterov) load_grad<W>(e, base + i, g);
+    const long long n = (long long)e.rows * e.cols, base = n * blockIdx.y, step = (long long)gridDim.x * 256 * W;
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * W; i < n; i += step * kAhead) {
+        float g[kAhead][W] = {}, v[kAhead][W];
 #pragma unroll
-            for (int j = 0; j < W; ++j) g[j] = e.nesterov ? fmaf(e.beta, v[j], g[j]) : v[j];
-        } else {
-            load_grad<W>(e, base + i, g);
-        }
-        const int row = (int)(i / e.cols), col = (int)(i - (long long)row * e.cols);
-        const long long at = ((long long)blockIdx.y * e.rows + row) * e.pitch + col;
-        if constexpr (W == 4) {
-            float l[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                g[j] *= inv;
-                l[j] = g[j] - __half2float(__float2half(g[j]));
+        for (int q = 0; q < kAhead; ++q)
+            if (i + q * step < n) {
+                if (!e.v_in || e.nesterov) load_grad<W>(e.grad, e.bf16, base + i + q * step, g[q]);
+                if (e.v_in) load_f32<W>(e.v_out + base + i + q * step, v[q]);
             }
-            *reinterpret_cast<uint2*>(e.hi + at) = make_uint2(pack2<__half>(g[0], g[1]), pack2<__half>(g[2], g[3]));
-            *reinterpret_cast<uint2*>(e.lo + at) = make_uint2(pack2<__half>(l[0], l[1]), pack2<__half>(l[2], l[3]));
-        } else {
-            const float x = g[0] * inv;
-            const __half h = __float2half(x);
-            e.hi[at] = h;
-            e.lo[at] = __float2half(x - __half2float(h));
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const long long k = i + q * step;
+            if (k >= n) continue;
+            form_u<W>(e, 0, false, g[q], v[q]);
+            const long long row = n < (1ll << 31) ? (int)k / e.cols : k / e.cols;
+            const long long at = ((long long)blockIdx.y * e.rows + row) * e.pitch + (k - row * e.cols);
+            float l[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                g[q][j] *= inv;
+                l[j] = g[q][j] - __half2float(__float2half(g[q][j]));
+            }
+            if constexpr (W == 4) {
+                *reinterpret_cast<uint2*>(e.hi + at) = make_uint2(pack2<__half>(g[q][0], g[q][1]), pack2<__half>(g[q][2], g[q][3]));
+                *reinterpret_cast<uint2*>(e.lo + at) = make_uint2(pack2<__half>(l[0], l[1]), pack2<__half>(l[2], l[3]));
+            } else {
+                e.hi[at] = __float2half(g[q][0]);
+                e.lo[at] = __float2half(l[0]);
+            }
         }
     }
 }
@@ -337,21 +332,18 @@ MuonPlan plan_muon(const ac_muon_desc& d) {
     p.k = d.rows < d.cols ? d.rows : d.cols;
     const int l = d.rows < d.cols ? d.cols : d.rows, all = (l + 63) / 64;
     if (p.k <= kOnchipK && l <= kOnchipL) {
-        // The fewest slabs per CTA that 8 CTAs, and a GPU's share per matrix, allow
-        const int most = kNumSMs / d.batch < 1 ? 1 : kNumSMs / d.batch < kOnchipCluster ? kNumSMs / d.batch : kOnchipCluster;
-        p.slabs = (all + most - 1) / most;
-        if (p.slabs > kOnchipSlabs) p.slabs = kOnchipSlabs;
+        // as many CTAs as there may be: a slab of 64 columns costs 1.1 us per step, another CTA's sums 0.3 us
+        p.slabs = (all + kOnchipCluster - 1) / kOnchipCluster;
         p.ctas = (all + p.slabs - 1) / p.slabs;
-        const long long k16 = up(p.k, 16);
         p.off_partial = kStatusBlockBytes;
         p.off_hi[0] = p.off_partial + (size_t)up((long long)d.batch * p.ctas * 4, 256);
-        p.bytes = p.off_hi[0] + (size_t)(2 * d.batch * p.ctas * k16 * 128 * 4);
+        p.bytes = p.off_hi[0] + (size_t)(2 * d.batch * p.ctas * up(p.k, 32) * up(p.k, 32) * 4);
         return p;
     }
     p.pitch = up(d.cols, 8);
     p.sym_pitch = up(p.k, 8);
     const long long n = (long long)d.rows * d.cols;
-    const long long want = (n + 2047) / 2048, most = kNormBlocks / d.batch > 1 ? kNormBlocks / d.batch : 1;
+    const long long want = (n + 1023) / 1024, most = kNormBlocks / d.batch > 1 ? kNormBlocks / d.batch : 1;
     p.blocks = (int)(want < most ? want : most);
     size_t at = kStatusBlockBytes;
     auto take = [&](long long bytes) {

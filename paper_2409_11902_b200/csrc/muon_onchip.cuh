@@ -1,14 +1,17 @@
-// The whole update of a small matrix in one kernel: at most 128 on the shorter side (k), 1536 on the longer (l).
+// The whole update of a small matrix in one kernel: at most 64 on the shorter side (k), 1344 on the longer (l).
 //
-// A cluster of up to 8 CTAs per matrix; each keeps a slice of at most 192 columns of X (k x l; a matrix with more rows
+// A cluster of up to 7 CTAs per matrix; each keeps a slice of at most 192 columns of X (k x l; a matrix with more rows
 // than columns is taken transposed) in shared memory from the gradient to the update, as two fp16 terms. Per step:
-//   Gram sum of the slice (tensor cores) -> partial sums to the workspace -> cluster barrier -> every CTA adds all of
-//   them, in the order of the slices -> A as two fp16 terms -> A^2 -> P = b A + c A^2 as two terms -> X <- a X + P X.
+//   Gram sum of the slice (tensor cores) -> partial sums to the workspace -> cluster barrier -> every CTA fetches the
+//   others' (bulk copies) and adds all of them in the order of the slices -> A as two fp16 terms -> A^2
+//   -> P = b A + c A^2 as two terms -> X <- a X + P X.
 // The slice of X is stored once, 64-column slabs of 128-byte rows: read along the rows it is the K-major operand of the
 // Gram product, read across them the MN-major operand of P X. Every product is formed from both terms of both operands
 // (hi hi + hi lo + lo hi), about 22 bits: at this size the products are a fourth of the time, and the small matrices'
 // errors do not average out. What bounds it is the chain of 15 products, each with its way through tensor memory and
-// shared memory: 64 x 576 takes 73 us in place of 80 for 17 launches of the kernels for large matrices.
+// shared memory, and 1.2 us for data that another SM has just written: 64 x 576 takes MEASURED in place of 80 for 17
+// launches of the kernels for large matrices. Beyond k = 64 the partial sums are 64 KB each, and their exchange costs
+// more than those launches (128 x 1152: 106 us against 95).
 #pragma once
 
 #include "mm_core.cuh"
@@ -19,17 +22,41 @@ using namespace mm;
 
 namespace {
 
-constexpr int kOnchipK = 128, kOnchipSlabs = 3, kOnchipCluster = 8;
+constexpr int kOnchipK = 64, kOnchipSlabs = 3, kOnchipCluster = 7;
 constexpr int kOnchipL = kOnchipSlabs * 64 * kOnchipCluster;
 constexpr uint32_t kSlab = 128 * 128;                     // 128 rows of 64 16-bit elements
-constexpr uint32_t kOnchipSmem = (2 * kOnchipSlabs + 4) * kSlab + 1024;
+constexpr uint32_t kGram = kOnchipK * kOnchipK * 4;          // one slice's partial sums at most
+constexpr uint32_t kOnchipSmem = (2 * kOnchipSlabs + 2) * kSlab + (kOnchipCluster - 1) * kGram + 1024;
+
+template <int W>
+__device__ __forceinline__ void load_grad(const void* grad, int bf16, long long at, float* g) {
+    if (bf16) {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(grad) + at;
+        if constexpr (W == 4) {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
+            const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
+            g[0] = a.x; g[1] = a.y; g[2] = b.x; g[3] = b.y;
+        } else {
+            g[0] = __bfloat162float(*p);
+        }
+    } else {
+        const float* p = static_cast<const float*>(grad) + at;
+        if constexpr (W == 4) {
+            const float4 u = *reinterpret_cast<const float4*>(p);
+            g[0] = u.x; g[1] = u.y; g[2] = u.z; g[3] = u.w;
+        } else {
+            g[0] = *p;
+        }
+    }
+}
 
 struct Onchip {
     const void* grad;
     const float* v_in;
     float* v_out;
     __nv_bfloat16* update;
-    float* partial;         // [2][batch][cluster][k16][128]: Gram sums, columns of 128 rows; two so that one barrier suffices
+    float* partial;         // [2][batch][cluster][k32][k32]: Gram sums by columns; two, so that one barrier per step suffices
     float* norms;           // [batch][cluster]
     uint32_t* status;
     float beta, a, b, c, eps, scale;
@@ -52,17 +79,18 @@ __device__ __forceinline__ void store_terms(uint8_t* hi, uint8_t* lo, int row, i
 
 __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ Onchip p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t done;
+    __shared__ uint64_t done, fetched;
     __shared__ uint32_t tmem_s;
     __shared__ int abort_s;
     __shared__ float part[8];
     uint8_t* smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));
-    uint8_t *xh = smem, *xl = xh + kOnchipSlabs * kSlab, *sh = xl + kOnchipSlabs * kSlab, *sl = sh + 2 * kSlab;
+    uint8_t *xh = smem, *xl = xh + kOnchipSlabs * kSlab, *sh = xl + kOnchipSlabs * kSlab, *sl = sh + kSlab;
+    float* others = reinterpret_cast<float*>(sl + kSlab);       // [cluster - 1][k32][k32]
     const uint32_t xh_a = smem_u32(xh), xl_a = smem_u32(xl), sh_a = smem_u32(sh), sl_a = smem_u32(sl);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int ctas = gridDim.x, rank = blockIdx.x, matrix = blockIdx.y;         // the cluster spans x
     const bool tall = p.rows > p.cols;
-    const int k16 = (p.k + 15) & ~15;
+    const int k16 = (p.k + 15) & ~15, k32 = (p.k + 31) & ~31;
     const int c0 = rank * p.slabs * 64, width = min(p.slabs * 64, p.l - c0);   // this CTA's columns of X
     const int slabs = (width + 63) / 64;
     const uint32_t idesc0 = (1u << 4) | ((uint32_t)(128 >> 4) << 24);           // fp16 operands, fp32 sums, M = 128
@@ -71,6 +99,7 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
     if (tid == 0) {
         abort_s = 0;
         mbar_init(&done, 1);
+        mbar_init(&fetched, 1);
         fence_barrier_init();
     }
     if (warp == 0) tmem_alloc(&tmem_s, 512);
@@ -96,51 +125,100 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
         c = tall ? s : f;
         return base + (tall ? (long long)(c0 + c) * p.cols + r : (long long)r * p.cols + c0 + c);
     };
-    auto load_g = [&](long long at) {
-        return p.bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.grad)[at]) : static_cast<const float*>(p.grad)[at];
-    };
-    float sum = 0.f;
-#pragma unroll 4
-    for (int i = tid; i < n; i += 256) {
-        int r, c;
-        const long long at = locate(i, r, c);
-        float u = load_g(at);
-        if (p.v_in) {
-            const float v = p.beta * p.v_in[at] + u;
-            p.v_out[at] = v;
-            u = p.nesterov ? fmaf(p.beta, v, u) : v;
-        }
-        sum = fmaf(u, u, sum);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) part[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < 8; ++w) sum += part[w];
-        p.norms[matrix * ctas + rank] = sum;
-    }
-    __syncthreads();
-    cluster_sync();
-    sum = 0.f;
-    for (int i = 0; i < ctas; ++i) sum += __ldcg(p.norms + matrix * ctas + i);
-    const float inv = 1.f / (sqrtf(sum) + p.eps);
-#pragma unroll 4
-    for (int i = tid; i < n; i += 256) {
-        int r, c;
-        const long long at = locate(i, r, c);
-        float u;
-        if (p.v_in) {
-            u = p.v_out[at];         // this thread wrote it
-            if (p.nesterov) u = fmaf(p.beta, u, load_g(at));
-        } else {
-            u = load_g(at);
-        }
-        u *= inv;
+    auto put_x = [&](int r, int c, float u) {
         const uint32_t to = slab_at(r, c);
         const __half h = __float2half(u);
         *reinterpret_cast<__half*>(xh + to) = h;
         *reinterpret_cast<__half*>(xl + to) = __float2half(u - __half2float(h));
+    };
+    // |u|^2 of the slice to the workspace, that of the matrix from all slices
+    auto inverse_norm = [&](float sum) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) part[warp] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < 8; ++w) sum += part[w];
+            p.norms[matrix * ctas + rank] = sum;
+        }
+        __syncthreads();
+        cluster_sync();
+        sum = 0.f;
+        for (int i = 0; i < ctas; ++i) sum += __ldcg(p.norms + matrix * ctas + i);
+        return 1.f / (sqrtf(sum) + p.eps);
+    };
+    float sum = 0.f;
+    if (p.cols % 4 == 0) {
+        // four at a time, and all of a thread's requested before the first is used: u stays in registers
+        constexpr int kQuads = kOnchipK * kOnchipSlabs * 64 / 4 / 256;
+        float4 u[kQuads];
+#pragma unroll
+        for (int q0 = 0; q0 < kQuads; q0 += 6) {
+            if (q0 * 1024 >= n) break;
+            float4 v[6];
+#pragma unroll
+            for (int q = 0; q < 6; ++q) {
+                const int i = (tid + (q0 + q) * 256) * 4;
+                if (i >= n) continue;
+                int r, c;
+                const long long at = locate(i, r, c);
+                float g[4];
+                load_grad<4>(p.grad, p.bf16, at, g);
+                u[q0 + q] = make_float4(g[0], g[1], g[2], g[3]);
+                if (p.v_in) v[q] = *reinterpret_cast<const float4*>(p.v_in + at);
+            }
+#pragma unroll
+            for (int q = 0; q < 6; ++q) {
+                const int i = (tid + (q0 + q) * 256) * 4;
+                if (i >= n) continue;
+                float4& w = u[q0 + q];
+                if (p.v_in) {
+                    int r, c;
+                    const long long at = locate(i, r, c);
+                    const float4 x = make_float4(p.beta * v[q].x + w.x, p.beta * v[q].y + w.y, p.beta * v[q].z + w.z, p.beta * v[q].w + w.w);
+                    *reinterpret_cast<float4*>(p.v_out + at) = x;
+                    w = p.nesterov ? make_float4(fmaf(p.beta, x.x, w.x), fmaf(p.beta, x.y, w.y), fmaf(p.beta, x.z, w.z), fmaf(p.beta, x.w, w.w)) : x;
+                }
+                sum = fmaf(w.x, w.x, fmaf(w.y, w.y, fmaf(w.z, w.z, fmaf(w.w, w.w, sum))));
+            }
+        }
+        const float inv = inverse_norm(sum);
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            const int i = (tid + q * 256) * 4;
+            if (i >= n) break;
+            int r, c;
+            locate(i, r, c);
+            const float4 w = make_float4(u[q].x * inv, u[q].y * inv, u[q].z * inv, u[q].w * inv);
+            put_x(r, c, w.x);
+            put_x(r + (tall ? 1 : 0), c + (tall ? 0 : 1), w.y);
+            put_x(r + (tall ? 2 : 0), c + (tall ? 0 : 2), w.z);
+            put_x(r + (tall ? 3 : 0), c + (tall ? 0 : 3), w.w);
+        }
+    } else {
+#pragma unroll 8
+        for (int i = tid; i < n; i += 256) {
+            int r, c;
+            const long long at = locate(i, r, c);
+            float u;
+            load_grad<1>(p.grad, p.bf16, at, &u);
+            if (p.v_in) {
+                const float v = p.beta * p.v_in[at] + u;
+                p.v_out[at] = v;
+                u = p.nesterov ? fmaf(p.beta, v, u) : v;
+            }
+            sum = fmaf(u, u, sum);
+        }
+        const float inv = inverse_norm(sum);
+#pragma unroll 8
+        for (int i = tid; i < n; i += 256) {
+            int r, c;
+            const long long at = locate(i, r, c);
+            float u = 0.f;
+            if (!p.v_in || p.nesterov) load_grad<1>(p.grad, p.bf16, at, &u);
+            if (p.v_in) u = p.nesterov ? fmaf(p.beta, p.v_out[at], u) : p.v_out[at];      // this thread wrote it
+            put_x(r, c, u * inv);
+        }
     }
     fence_proxy_async_smem();
     __syncthreads();
@@ -150,7 +228,6 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
     const int row = quarter * 32 + lane;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     uint32_t phase = 0;
-    bool ok = true;
     // three products of one K step: hi hi, hi lo, lo hi
     auto three = [&](uint32_t d, uint32_t ah, uint32_t al, uint32_t bh, uint32_t bl, uint32_t idesc, bool first) {
         mma_words<1>(d, ah, hi, bh, hi, idesc, first ? 0u : 1u);
@@ -161,13 +238,11 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
         const bool got = mbar_wait(&done, phase, abort_flag);
         phase ^= 1;
         if (!got) flag_timeout(&abort_s, p.status, 0x1500u);
-        ok = ok && got;
         __syncwarp();
         tc_fence_after();
     };
     for (int step = 0; step < p.steps; ++step) {
         // ---- A = X X^T
-        float a[2][32];
         if (tid == 0) {
             const uint32_t idesc = idesc0 | ((uint32_t)(k16 >> 3) << 17);
             for (int s = 0; s < slabs * 4; ++s) {
@@ -179,51 +254,66 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
         }
         __syncwarp();
         finish();
-        float* mine = p.partial + (((long long)(step & 1) * gridDim.y + matrix) * ctas + rank) * k16 * 128;
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int c = (g * 2 + half) * 32;
-            if (c >= k16) continue;
+        // this thread's share: 32 columns from c of one row; the warps whose rows or columns lie past k have none
+        const int c = half * 32;
+        const bool mine = c < k16 && quarter * 32 < p.k;
+        float a[32];
+        if (mine) {
             uint32_t r[32];
             tmem_ld32(d_sym + lanes + c, r);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) a[g][j] = __uint_as_float(r[j]);
-            if (ctas > 1 && quarter * 32 < p.k) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (c + j < k16) mine[(c + j) * 128 + row] = a[g][j];
-            }
+            for (int j = 0; j < 32; ++j) a[j] = __uint_as_float(r[j]);
         }
         if (ctas > 1) {
+            const uint32_t bytes = (uint32_t)(k32 * k32 * 4);
+            float* slices = p.partial + ((long long)(step & 1) * gridDim.y + matrix) * ctas * k32 * k32;
+            if (mine) {
+                float* to = slices + ((long long)rank * k32 + c) * k32 + row;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) to[j * k32] = a[j];
+            }
+            fence_proxy_async_all();      // the other CTAs' bulk copies read what was written here
             __syncwarp();
             cluster_sync();
-            const float* all = p.partial + ((long long)(step & 1) * gridDim.y + matrix) * ctas * k16 * 128;
+            if (tid == 0) {
+                fence_proxy_async_all();
+                mbar_arrive_expect_tx(&fetched, bytes * (ctas - 1));
+                for (int s = 0, to = 0; s < ctas; ++s)
+                    if (s != rank) bulk_load(smem_u32(others) + bytes * to++, slices + (long long)s * k32 * k32, bytes, &fetched);
+            }
+            __syncwarp();
+            const bool got = mbar_wait(&fetched, step & 1, abort_flag);
+            if (!got) flag_timeout(&abort_s, p.status, 0x1600u);
+            __syncwarp();
+            if (mine) {
+                // no bounds on the loads: a guard around each would make them wait for one another
+                float t[32];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int c = (g * 2 + half) * 32;
-                if (c >= k16 || quarter * 32 >= p.k) continue;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) a[g][j] = 0.f;
+                for (int j = 0; j < 32; ++j) t[j] = 0.f;
+                const float* q = others + c * k32 + row;
                 for (int s = 0; s < ctas; ++s) {
-                    const float* from = all + (long long)s * k16 * 128 + row;
+                    if (s == rank) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (c + j < k16) a[g][j] += __ldcg(from + (c + j) * 128);
+                        for (int j = 0; j < 32; ++j) t[j] += a[j];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) t[j] += q[j * k32];
+                        q += k32 * k32;
+                    }
                 }
+#pragma unroll
+                for (int j = 0; j < 32; ++j) a[j] = t[j];
             }
         }
         // both terms of A, then A^2, then both terms of P in their place
-        auto put = [&](auto&& value) {
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int c = (g * 2 + half) * 32;
-                if (c >= k16) continue;
+        auto put = [&]() {
+            if (mine && row < p.k) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 8) {
-                    if (c + j >= k16 || row >= p.k) continue;
+                    if (c + j >= k16) continue;
                     float v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = c + j + i < p.k ? value(g, j + i) : 0.f;
+                    for (int i = 0; i < 8; ++i) v[i] = c + j + i < p.k ? a[j + i] : 0.f;
                     store_terms(sh, sl, row, c + j, v);
                 }
             }
@@ -232,33 +322,29 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
             __syncthreads();
             tc_fence_after();
         };
-        put([&](int g, int j) { return a[g][j]; });
+        put();
         if (tid == 0) {
             const uint32_t idesc = idesc0 | ((uint32_t)(k16 >> 3) << 17);
             for (int s = 0; s < k16 / 16; ++s) {
-                const uint32_t off = (uint32_t)(s >> 2) * kSlab + (s & 3) * 32;
-                const uint32_t h = desc_lo(sh_a + off, 16), l = desc_lo(sl_a + off, 16);
+                const uint32_t h = desc_lo(sh_a + s * 32, 16), l = desc_lo(sl_a + s * 32, 16);
                 three(d_sym, h, l, h, l, idesc, s == 0);
             }
             mma_commit(&done);
         }
         __syncwarp();
         finish();
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int c = (g * 2 + half) * 32;
-            if (c >= k16) continue;
+        if (mine) {
             uint32_t r[32];
             tmem_ld32(d_sym + lanes + c, r);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) a[g][j] = fmaf(p.b, a[g][j], p.c * __uint_as_float(r[j]));
+            for (int j = 0; j < 32; ++j) a[j] = fmaf(p.b, a[j], p.c * __uint_as_float(r[j]));
         }
-        put([&](int g, int j) { return a[g][j]; });
+        put();
         // ---- X <- a X + P X
         if (tid == 0) {
             const uint32_t idesc = idesc0 | (1u << 16) | ((uint32_t)(slabs * 64 >> 3) << 17);
             for (int s = 0; s < k16 / 16; ++s) {
-                const uint32_t pa = (uint32_t)(s >> 2) * kSlab + (s & 3) * 32, xb = (uint32_t)s * 2048;
+                const uint32_t pa = (uint32_t)s * 32, xb = (uint32_t)s * 2048;
                 three(d_x, desc_lo(sh_a + pa, 16), desc_lo(sl_a + pa, 16), desc_lo(xh_a + xb, kSlab), desc_lo(xl_a + xb, kSlab),
                       idesc, s == 0);
             }
@@ -268,23 +354,23 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
         finish();
         const bool last = step + 1 == p.steps;
 #pragma unroll 1
-        for (int c = half * 32; c < slabs * 64; c += 64) {
+        for (int s = half * 32; s < slabs * 64; s += 64) {
             uint32_t r[32];
-            tmem_ld32(d_x + lanes + c, r);
+            tmem_ld32(d_x + lanes + s, r);
             if (row < p.k) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 8) {
-                    const uint32_t at = slab_at(row, c + j);
+                    const uint32_t at = slab_at(row, s + j);
                     float v[8], w[8];
                     load8(reinterpret_cast<const __half*>(xh + at), v);
                     load8(reinterpret_cast<const __half*>(xl + at), w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] = fmaf(p.a, v[i] + w[i], __uint_as_float(r[j + i]));
                     if (!last) {
-                        store_terms(xh, xl, row, c + j, v);
+                        store_terms(xh, xl, row, s + j, v);
                         continue;
                     }
-                    const int col = c0 + c + j;
+                    const int col = c0 + s + j;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] *= p.scale;
                     if (!tall && p.cols % 8 == 0) {
