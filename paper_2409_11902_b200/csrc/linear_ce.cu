@@ -5,13 +5,16 @@
 //   g_tv   = dloss_t (exp(l_tv - lse_t) - [v = y(t)])
 //   dh = g w       dw = g^T h       db_v = sum_t g_tv
 //
-// The classes are taken in pieces of `width` columns. The logits kernel leaves, per row and per 64 or 128 columns, the
-// maximum m and s = sum exp(l - m), both fp32, and nothing else; a small kernel joins them to lse. The
+// The classes are taken in pieces of `width` columns. The logits kernel leaves, per row and per block of 32, 64 or 128
+// columns, the maximum m and s = sum exp(l - m), both fp32, and nothing else; a small kernel joins them to lse. The
 // gradient of a piece is formed by a second product over the piece (its epilogue writes g in the inputs' type), from
 // which come the piece's rows of dw and its share of dh (summed over the pieces in fp32). For the last piece the
 // second product is not needed: the logits kernel leaves e = exp(l - m) of that piece as fp16 (11 bits over a range of
 // 2^40 below the maximum of its block of columns), and g = dloss e exp(m - lse) is one pass over the piece. With room for
 // all V columns there is one piece and three products in all, as many as the formulas have.
+// g is kept divided by the largest |dloss|, which the gradients' epilogues multiply in again: with the weights of a mean
+// the entry of almost every label is close to -1 / count, and rounding that same number to bf16 over and over would bias
+// the sums (backward at 4096 x 65536: 3.0e-3 off; divided 2.2e-3, the two roundings' own share).
 #include "mm_core.cuh"
 
 namespace ac {
@@ -36,6 +39,8 @@ struct Ce {
     int first;                   // first class of this piece
     int width;                   // classes of this piece
     int block;                   // columns that share one (m, s): the half tile of one epilogue warp
+    float* top;                  // the largest |dloss| of the tokens that count
+    float* columns;              // [ceil(T/32)][pitch]: column sums of g over 32 rows each, or null
 };
 
 __device__ __forceinline__ bool live(long long label, int classes) { return label >= 0 && label < classes; }
@@ -61,14 +66,29 @@ __device__ __forceinline__ void logits32(const Ce& c, uint32_t taddr, int col, f
     }
 }
 
-// Statistics of a row's 128 columns; KEEP: and exp(l - m) as fp16.
+// Sums over the 32 rows of a warp of 32 columns that each thread holds of its row: thread j gets column j.
+__device__ __forceinline__ float warp_columns(float (&x)[32], int lane) {
+#pragma unroll
+    for (int n = 16; n > 0; n >>= 1) {
+        const bool upper = lane & n;
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+            const float give = upper ? x[j] : x[j + n], keep = upper ? x[j + n] : x[j];
+            x[j] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+        }
+    }
+    return x[0];
+}
+
+// Statistics of a row's COLS columns; KEEP: and exp(l - m) as fp16.
 template <bool KEEP>
 struct StatsEpi : Ce {
     static constexpr bool kWholeRow = true;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
-    __device__ __forceinline__ void row(uint32_t taddr, int t, int col) const {
+    __device__ __forceinline__ void row(uint32_t taddr, int row0, int lane, int col, uint8_t* patch) const {
+        const int t = row0 + lane;
         const bool in = t < tokens;
         const int label = [&] {
             const long long y = in ? labels[t] : -1;
@@ -100,14 +120,10 @@ struct StatsEpi : Ce {
                 sum[j & 3] += x[j];
             }
             if constexpr (KEEP) {
-                if (in && col + c < pitch) {
-                    // 2^15 times e: what lies 2^29 and more below the block's maximum loses bits, not what matters
+                // 2^15 times e: what lies 2^29 and more below the block's maximum loses bits, not what matters
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] *= 32768.f;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8)
-                        if (col + c + j < pitch) store8(e + (long long)t * pitch + col + c + j, x + j);
-                }
+                for (int j = 0; j < 32; ++j) x[j] *= 32768.f;
+                store_rows(e + (long long)row0 * pitch + col + c, pitch, tokens - row0, (int)pitch - col - c, x, patch, lane);
             }
         }
         if (in && col < width)
@@ -121,11 +137,12 @@ struct GradEpi : Ce {
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
-    __device__ __forceinline__ void row(uint32_t taddr, int t, int col) const {
+    __device__ __forceinline__ void row(uint32_t taddr, int row0, int lane, int col, uint8_t* patch) const {
+        const int t = row0 + lane;
         const bool in = t < tokens;
         const long long y = in ? labels[t] : -1;
         const bool counts = live(y, classes);
-        const float scale = counts ? dloss[t] : 0.f, shift = counts ? lse[t] : 0.f;
+        const float scale = counts ? dloss[t] / *top : 0.f, shift = counts ? lse[t] : 0.f;
         const int label = counts && y >= first + col && y < first + col + COLS ? (int)(y - first) : -1;
 #pragma unroll 1
         for (int c = 0; c < COLS; c += 32) {
@@ -138,10 +155,10 @@ struct GradEpi : Ce {
                 for (int j = 0; j < 32; ++j)
                     if (label == col + c + j) x[j] -= scale;
             }
-            if (in) {
-#pragma unroll
-                for (int j = 0; j < 32; j += 8)
-                    if (col + c + j < pitch) store8(g + (long long)t * pitch + col + c + j, x + j);
+            store_rows(g + (long long)row0 * pitch + col + c, pitch, tokens - row0, (int)pitch - col - c, x, patch, lane);
+            if (columns) {
+                const float v = warp_columns(x, lane);
+                if (row0 < tokens && col + c + lane < width) columns[(long long)(row0 / 32) * pitch + col + c + lane] = v;
             }
         }
     }
@@ -152,6 +169,7 @@ struct OutEpi {
     static constexpr bool kWholeRow = false, kMirror = false, kScalar = true;
     __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
     float* sum;             // [rows][pitch], or null
+    const float* top;       // what g was divided by
     int add;                // 1: what earlier pieces left in `sum` is added
     int rows, cols, pitch;
     __device__ __forceinline__ bool scalar() const { return out && cols % 8 != 0; }
@@ -181,104 +199,208 @@ struct OutEpi {
                 v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
                 v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
             }
-            if (!out) {
+            if (out) {
+                const float scale = *top;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] *= scale;
+                if (cols % 8 == 0) store8(out + (long long)row * cols + col, v[i]);
+            } else {
                 float4* q = reinterpret_cast<float4*>(sum + (long long)row * pitch + col);
                 q[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
                 q[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
-            } else if (cols % 8 == 0) {
-                store8(out + (long long)row * cols + col, v[i]);
             }
         }
     }
 };
 
-// Joins a row's statistics: lse and loss. 8 rows per block; 32 threads share a row's blocks of columns.
-__global__ void __launch_bounds__(256) join_kernel(const float2* stats, int blocks, int tokens, int classes,
-                                                   const long long* labels, const float* at_label, float* lse, float* loss) {
+__device__ __forceinline__ void join_stats(float2& a, float2 o) {
+    // fmaxf drops a NaN maximum; the sum beside it is NaN then and carries it
+    const float top = fmaxf(a.x, o.x), keep = top == -INFINITY ? 0.f : top;
+    a.y = a.y * ex2((a.x - keep) * kLog2e) + o.y * ex2((o.x - keep) * kLog2e);
+    a.x = top;
+}
+
+// The largest finite |dloss| of the tokens that count, 1 if that is 0; called by all threads of a block.
+__device__ __forceinline__ float largest_weight(const float* dloss, const long long* labels, int tokens, int classes) {
+    __shared__ float part[32];
+    float m = 0.f;
+#pragma unroll 4
+    for (int t = threadIdx.x; t < tokens; t += blockDim.x) {
+        const float x = fabsf(dloss[t]);
+        if (live(labels[t], classes) && x < INFINITY) m = fmaxf(m, x);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = part[0];
+    for (int w = 1; w < blockDim.x / 32; ++w) m = fmaxf(m, part[w]);
+    return m > 0.f ? m : 1.f;
+}
+__global__ void __launch_bounds__(1024) weight_kernel(Ce c) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const float m = largest_weight(c.dloss, c.labels, c.tokens, c.classes);
+    if (threadIdx.x == 0) *c.top = m;
+}
+
+// Joins a row's statistics: lse and loss. 8 rows per block; 32 threads share a row's blocks of columns. With dloss, one
+// block more finds the largest weight.
+__global__ void __launch_bounds__(256) join_kernel(Ce c, int blocks, float* lse, float* loss) {
     __shared__ float2 part[32][8];
     pdl_launch_dependents();
     pdl_wait();
+    if (c.dloss && blockIdx.x == gridDim.x - 1) {
+        const float m = largest_weight(c.dloss, c.labels, c.tokens, c.classes);
+        if (threadIdx.x == 0) *c.top = m;
+        return;
+    }
     const int r = threadIdx.x & 7, slice = threadIdx.x >> 3, t = blockIdx.x * 8 + r;
-    float m = -INFINITY, s = 0.f;
-    auto add = [&](float2 o) {
-        // fmaxf drops a NaN maximum; the sum beside it is NaN then and carries it
-        const float top = fmaxf(m, o.x), keep = top == -INFINITY ? 0.f : top;
-        s = s * ex2((m - keep) * kLog2e) + o.y * ex2((o.x - keep) * kLog2e);
-        m = top;
-    };
-    if (t < tokens) {
+    float2 a = make_float2(-INFINITY, 0.f);
+    if (t < c.tokens) {
         int b = slice;
         for (; b + 96 < blocks; b += 128) {
             float2 x[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = stats[(long long)(b + 32 * i) * tokens + t];
+            for (int i = 0; i < 4; ++i) x[i] = c.stats[(long long)(b + 32 * i) * c.tokens + t];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) add(x[i]);
+            for (int i = 0; i < 4; ++i) join_stats(a, x[i]);
         }
-        for (; b < blocks; b += 32) add(stats[(long long)b * tokens + t]);
+        for (; b < blocks; b += 32) join_stats(a, c.stats[(long long)b * c.tokens + t]);
     }
-    part[slice][r] = make_float2(m, s);
+    part[slice][r] = a;
     __syncthreads();
-    if (threadIdx.x < 8 && t < tokens) {
-        for (int w = 1; w < 32; ++w) add(part[w][r]);
-        const float l = m + logf(s);
+    if (threadIdx.x < 8 && t < c.tokens) {
+        for (int w = 1; w < 32; ++w) join_stats(a, part[w][r]);
+        const float l = a.x + logf(a.y);
         lse[t] = l;
-        loss[t] = live(labels[t], classes) ? l - at_label[t] : 0.f;
+        loss[t] = live(c.labels[t], c.classes) ? l - c.at_label[t] : 0.f;
     }
 }
 
-// The kept piece: g = dloss exp(l - m) exp(m - lse), in place over e; the label's entry from its own fp32 logit.
-__global__ void __launch_bounds__(256) kept_kernel(Ce c, const float* at_label) {
-    pdl_launch_dependents();
-    pdl_wait();
-    const int t = blockIdx.x, per_row = (int)(c.pitch / 8);
-    const long long y = c.labels[t];
-    const bool counts = live(y, c.classes);
-    const float lse = c.lse[t], dl = counts ? c.dloss[t] : 0.f;
-    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < per_row; i += gridDim.y * blockDim.x) {
-        const int col = i * 8;
-        const long long at = (long long)t * c.pitch + col;
-        float v[8];
-        load8(c.e + at, v);
-        const float m = col < c.width ? c.stats[(long long)((c.first + col) / c.block) * c.tokens + t].x : lse;
-        const float f = m == -INFINITY ? 0.f : ex2((m - lse) * kLog2e) * (1.f / 32768.f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = counts && col + j < c.width ? v[j] * f * dl : 0.f;
-        if (counts && y >= c.first + col && y < c.first + col + 8) {
-            const float p = ex2((at_label[t] - lse) * kLog2e);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c.first + col + j == y) v[j] = dl * (p - 1.f);
-        }
-        store8(c.g + at, v);
-    }
-}
-
-// db of a piece: column sums of g in fp32, 64 columns per block, rows in a fixed order.
-__global__ void __launch_bounds__(256) column_sum_kernel(const __nv_bfloat16* g, long long pitch, int tokens, int width,
-                                                         __nv_bfloat16* out) {
+// The kept piece: g = dloss exp(l - m) exp(m - lse), in place over e; the label's entry from its own fp32 logit. A block
+// takes 32 rows of 256 columns. JOIN: few tokens and classes, so every block joins its rows' statistics itself.
+constexpr int kJoinTokens = 1024, kJoinClasses = 4096;
+template <bool JOIN>
+__global__ void __launch_bounds__(256) kept_kernel(Ce c, int blocks, float* lse_out, float* loss_out) {
+    __shared__ float sums[8][256];
     __shared__ float2 part[8][32];
+    __shared__ float row_lse[32], row_weight[32], row_p[32];
+    __shared__ int row_label[32];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 64 + lane * 2;
-    float2 s = make_float2(0.f, 0.f);
-    if (col < width) {
-#pragma unroll 4
-        for (int t = warp; t < tokens; t += 8) {
-            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(g + t * pitch + col));
-            s.x += f.x;
-            s.y += f.y;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row0 = blockIdx.x * 32, col = blockIdx.y * 256 + lane * 8;
+    float top;
+    if constexpr (JOIN) {
+        top = largest_weight(c.dloss, c.labels, c.tokens, c.classes);
+        if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *c.top = top;
+        float2 a = make_float2(-INFINITY, 0.f);
+        if (row0 + lane < c.tokens) {
+            int b = warp;
+            for (; b + 24 < blocks; b += 32) {
+                float2 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = c.stats[(long long)(b + 8 * i) * c.tokens + row0 + lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) join_stats(a, x[i]);
+            }
+            for (; b < blocks; b += 8) join_stats(a, c.stats[(long long)b * c.tokens + row0 + lane]);
         }
+        part[warp][lane] = a;
+        __syncthreads();
+    } else {
+        top = *c.top;
+    }
+    if (warp == 0) {
+        const int t = row0 + lane;
+        float lse = 0.f, weight = 0.f, p = 0.f;
+        int label = -1;
+        if (t < c.tokens) {
+            const long long y = c.labels[t];
+            const bool counts = live(y, c.classes);
+            if constexpr (JOIN) {
+                float2 a = part[0][lane];
+                for (int w = 1; w < 8; ++w) join_stats(a, part[w][lane]);
+                lse = a.x + logf(a.y);
+                if (blockIdx.y == 0) {
+                    lse_out[t] = lse;
+                    loss_out[t] = counts ? lse - c.at_label[t] : 0.f;
+                }
+            } else {
+                lse = c.lse[t];
+            }
+            if (counts) {
+                weight = c.dloss[t] / top;
+                if (y >= c.first && y < c.first + c.width) {
+                    label = (int)(y - c.first);
+                    p = ex2((c.at_label[t] - lse) * kLog2e);
+                }
+            } else {
+                label = -2;      // the row is zero, whatever its logits
+            }
+        }
+        row_lse[lane] = lse;
+        row_weight[lane] = weight;
+        row_p[lane] = p;
+        row_label[lane] = label;
+    }
+    __syncthreads();
+    float add[8] = {};
+    if (col < c.pitch) {
+        uint4 x[4];
+        float m[4];
+        const int b = min(c.first + col, c.first + c.width - 1) / c.block;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = min(row0 + warp + 8 * i, c.tokens - 1);
+            x[i] = *reinterpret_cast<const uint4*>(c.e + (long long)r * c.pitch + col);
+            m[i] = c.stats[(long long)b * c.tokens + r].x;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int l = warp + 8 * i, r = row0 + l, label = row_label[l];
+            if (r >= c.tokens) continue;
+            const float weight = row_weight[l];
+            const float f = m[i] == -INFINITY ? 0.f : ex2((m[i] - row_lse[l]) * kLog2e) * (1.f / 32768.f) * weight;
+            float v[8];
+            unpack8(x[i], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = label == -2 || col + j >= c.width ? 0.f : col + j == label ? (row_p[l] - 1.f) * weight : v[j] * f;
+                add[j] += v[j];
+            }
+            store8(c.g + (long long)r * c.pitch + col, v);
+        }
+    }
+    if (!c.columns) return;
+    *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(add[0], add[1], add[2], add[3]);
+    *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(add[4], add[5], add[6], add[7]);
+    __syncthreads();
+    const int at = blockIdx.y * 256 + threadIdx.x;
+    if (at < c.width) {
+        float t = sums[0][threadIdx.x];
+        for (int w = 1; w < 8; ++w) t += sums[w][threadIdx.x];
+        c.columns[(long long)blockIdx.x * c.pitch + at] = t;
+    }
+}
+
+// db of a piece from the sums over 32 rows each, first to last; 32 columns per block, 8 warps share the rows.
+__global__ void __launch_bounds__(256) column_kernel(Ce c, __nv_bfloat16* out) {
+    __shared__ float part[8][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, rows = (c.tokens + 31) / 32;
+    float s = 0.f;
+    if (col < c.width) {
+        const float* from = c.columns + col;
+#pragma unroll 8
+        for (int r = warp; r < rows; r += 8) s += from[r * c.pitch];
     }
     part[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && col < width) {
-        for (int w = 1; w < 8; ++w) {
-            s.x += part[w][lane].x;
-            s.y += part[w][lane].y;
-        }
-        out[col] = __float2bfloat16(s.x);
-        if (col + 1 < width) out[col + 1] = __float2bfloat16(s.y);
+    if (warp == 0 && col < c.width) {
+        for (int w = 1; w < 8; ++w) s += part[w][lane];
+        out[col] = __float2bfloat16(s * *c.top);
     }
 }
 
@@ -303,9 +425,10 @@ inline long long up(long long a, long long b) { return (a + b - 1) / b * b; }
 
 struct CePlan {
     int width, pieces;                      // columns of g held at a time; pieces of the classes
-    int block;                              // columns per entry of the statistics; 128: tiles of CTA pairs
+    Shape logits;                           // one for all pieces: half its tiles' width is the statistics' block
+    int block;
     long long pitch;
-    size_t off_stats, off_label, off_lse, off_sum, off_h, off_w, off_g, off_slices, slice_bytes, bytes;
+    size_t off_top, off_stats, off_label, off_sum, off_h, off_w, off_g, off_columns, off_slices, slice_bytes, bytes;
 };
 
 bool valid(const ac_linear_ce_desc* d) {
@@ -329,7 +452,9 @@ CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
         at += (size_t)up(bytes, 256);
         return o;
     };
-    p.block = shape(Problem{d.tokens, p.width, D, 1, true, false}, true, 0).pairs ? 128 : 64;
+    p.logits = shape(Problem{d.tokens, p.width, d.features, 1, true, false}, true, 0);
+    p.block = p.logits.bn / 2;
+    p.off_top = take(4);
     p.off_stats = take((V + p.block - 1) / p.block * T * 8);
     p.off_label = take(T * 4);
     if (D != Dp) {
@@ -339,6 +464,7 @@ CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
     if (grad) {
         if (p.pieces > 1) p.off_sum = take(T * Dp * 4);
         p.off_g = take(T * p.pitch * 2);
+        if (d.has_bias) p.off_columns = take((T + 31) / 32 * p.pitch * 4);
         const size_t dh = scratch_bytes(Problem{d.tokens, d.features, p.width, 1, true, false});
         const size_t dw = scratch_bytes(Problem{p.width < V ? p.width : (int)V, d.features, T, 1, true, false});
         p.slice_bytes = dh > dw ? dh : dw;
@@ -428,6 +554,8 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
     c.classes = V;
     c.pitch = p.pitch;
     c.block = p.block;
+    c.top = reinterpret_cast<float*>(ws + p.off_top);
+    c.columns = a.dbias ? reinterpret_cast<float*>(ws + p.off_columns) : nullptr;
     c.g = reinterpret_cast<__nv_bfloat16*>(ws + p.off_g);
 
     auto piece = [&](int i) {
@@ -436,7 +564,6 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
     };
     auto rows_of_w = [&] { return static_cast<const char*>(w) + (long long)c.first * Dp * 2; };
     const Operand H{h, D, T, Dp, 1, 0, false};
-    const Shape logits{p.block == 128, 1, false};      // one for all pieces: it sets the statistics' block
     ac_status rc;
     if (forward) {
         for (int i = 0; i < p.pieces; ++i) {
@@ -446,43 +573,45 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
             if (grad && i == p.pieces - 1) {
                 StatsEpi<true> e{c};
                 e.e = reinterpret_cast<__half*>(c.g);
-                rc = launch_shaped<false, false>(H, W, q, logits, call, e);
+                rc = launch_shaped<false, false>(H, W, q, p.logits, call, e);
             } else {
-                rc = launch_shaped<false, false>(H, W, q, logits, call, StatsEpi<false>{c});
+                rc = launch_shaped<false, false>(H, W, q, p.logits, call, StatsEpi<false>{c});
             }
             if (rc != AC_OK) return rc;
         }
-        AC_CUDA_TRY(launch_after(join_kernel, dim3((T + 7) / 8), dim3(256), 0, a.st,
-                                 static_cast<const float2*>(c.stats), (V + p.block - 1) / p.block, T, V, c.labels,
-                                 static_cast<const float*>(c.at_label), a.lse, a.loss));
     }
+    const int blocks = (V + p.block - 1) / p.block;
+    const bool joined = forward && grad && p.pieces == 1 && T <= kJoinTokens && V <= kJoinClasses;     // by kept_kernel
+    if (forward && !joined)
+        AC_CUDA_TRY(launch_after(join_kernel, dim3((T + 7) / 8 + (grad ? 1 : 0)), dim3(256), 0, a.st, c, blocks, a.lse, a.loss));
+    if (grad && !forward) AC_CUDA_TRY(launch_after(weight_kernel, dim3(1), dim3(1024), 0, a.st, c));
     if (!grad) return AC_OK;
     for (int i = p.pieces - 1; i >= 0; --i) {
         piece(i);
         if (forward && i == p.pieces - 1) {
             Ce k = c;
             k.e = reinterpret_cast<__half*>(c.g);
-            AC_CUDA_TRY(launch_after(kept_kernel, dim3(T, (unsigned)((p.pitch + 8191) / 8192)), dim3(256), 0, a.st, k,
-                                     static_cast<const float*>(c.at_label)));
+            AC_CUDA_TRY(launch_after(joined ? kept_kernel<true> : kept_kernel<false>,
+                                     dim3((T + 31) / 32, (unsigned)((p.pitch + 255) / 256)), dim3(256), 0, a.st, k, blocks, a.lse,
+                                     a.loss));
         } else {
             const Operand W{rows_of_w(), D, c.width, Dp, 1, 0, false};
-            rc = launch_shaped<false, false>(H, W, Problem{T, c.width, D, 1, true, false}, logits, call, GradEpi{c});
+            rc = launch_shaped<false, false>(H, W, Problem{T, c.width, D, 1, true, false}, p.logits, call, GradEpi{c});
             if (rc != AC_OK) return rc;
         }
         if (a.dbias)
-            AC_CUDA_TRY(launch_after(column_sum_kernel, dim3((c.width + 63) / 64), dim3(256), 0, a.st,
-                                     static_cast<const __nv_bfloat16*>(c.g), p.pitch, T, c.width,
+            AC_CUDA_TRY(launch_after(column_kernel, dim3((c.width + 31) / 32), dim3(256), 0, a.st, c,
                                      static_cast<__nv_bfloat16*>(a.dbias) + c.first));
         {   // rows of dw: g^T h
             const Operand G{c.g, c.width, T, p.pitch, 1, 0, true}, Ht{h, D, T, Dp, 1, 0, true};
-            const OutEpi e{static_cast<__nv_bfloat16*>(a.dw) + (long long)c.first * D, nullptr, 0, c.width, D, 0};
+            const OutEpi e{static_cast<__nv_bfloat16*>(a.dw) + (long long)c.first * D, nullptr, c.top, 0, c.width, D, 0};
             rc = launch<true, true>(G, Ht, Problem{c.width, D, T, 1, true, false}, call, e);
             if (rc != AC_OK) return rc;
         }
         {   // dh: g w, over this piece
             const Operand G{c.g, c.width, T, p.pitch, 1, 0, false}, Wt{rows_of_w(), D, c.width, Dp, 1, 0, true};
             const OutEpi e{i == 0 ? static_cast<__nv_bfloat16*>(a.dh) : nullptr,
-                           p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sum) : nullptr, i != p.pieces - 1, T, D, (int)Dp};
+                           p.pieces > 1 ? reinterpret_cast<float*>(ws + p.off_sum) : nullptr, c.top, i != p.pieces - 1, T, D, (int)Dp};
             rc = launch<false, true>(G, Wt, Problem{T, D, c.width, 1, true, false}, call, e);
             if (rc != AC_OK) return rc;
         }

@@ -11,12 +11,12 @@
 // other one is being filled (two accumulators of BN columns). Two shapes:
 //   CG = 2, BN = 256: a pair of SMs computes a 256 x 256 tile (cta_group::2); each holds 128 rows of A and 128 rows
 //           of B, so a K-tile costs 32 KB of shared memory per SM for twice the MMA work of a lone 128 x 128 tile.
-//   CG = 1, BN = 128: 128 x 128 tiles for problems with fewer than a GPU's worth of large tiles.
+//   CG = 1, BN = 128 or 64: 128 x 128 or 128 x 64 tiles for problems with fewer than a GPU's worth of large tiles.
 // Where the tiles are too few and K is long, K is cut into slices: each is a tile of its own that leaves fp32 sums in the
 // workspace, and a second kernel adds the slices in their order and applies the epilogue (a cluster that adds them up in
 // distributed shared memory was slower: that memory gives about 25 GB/s to an SM, the L2 three times as much).
-// K-tiles of 64 arrive at one per 0.27 us and SM for either shape (64 bytes per clock from the L2, or the MMAs of a pair);
-// shape() chooses shape and slices by that rate.
+// A K-tile of 64 takes an SM 0.27 us in the first two shapes (64 bytes per clock from the L2, or the MMAs of a pair) and
+// 0.20 us in the last; shape() chooses shape and slices by these rates.
 #pragma once
 
 #include <cuda.h>
@@ -37,6 +37,8 @@ constexpr int kBK = 64;                      // K-tile: one 128-byte swizzle row
 constexpr int kMaxStages = 6;
 constexpr int kPatchPitch = 36;              // floats between the rows of a warp's 32 x 32 patch: no bank conflicts
 constexpr int kPatchBytes = kEpiWarps * 32 * kPatchPitch * 4;
+constexpr int kRowPatch = 80;                // bytes between the rows of a warp's 32 x 32 patch of 16-bit values
+constexpr int kRowPatchBytes = kEpiWarps * 32 * kRowPatch;
 constexpr int kMaxSlices = 16;
 
 struct Params {
@@ -212,6 +214,26 @@ __device__ __forceinline__ void unpack8(const uint4& u, float* v) {
 }
 __device__ __forceinline__ void load8(const __half* src, float* v) { unpack8(*reinterpret_cast<const uint4*>(src), v); }
 
+// 32 x 32 values, 32 of a row per thread, to rows of 16-bit values: through a patch of shared memory, so that 4 threads
+// write 64 bytes of one row. `dst`: the first row's address of these columns; rows past `rows`, columns past `cols` are left out.
+template <class T>
+__device__ __forceinline__ void store_rows(T* dst, long long pitch, int rows, int cols, const float* x, uint8_t* patch, int lane) {
+    uint4* own = reinterpret_cast<uint4*>(patch + lane * kRowPatch);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        own[j] = make_uint4(pack2<T>(x[8 * j], x[8 * j + 1]), pack2<T>(x[8 * j + 2], x[8 * j + 3]),
+                            pack2<T>(x[8 * j + 4], x[8 * j + 5]), pack2<T>(x[8 * j + 6], x[8 * j + 7]));
+    __syncwarp();
+    const int c = (lane & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + (lane >> 2);
+        const uint4 v = *reinterpret_cast<const uint4*>(patch + r * kRowPatch + c * 2);
+        if (r < rows && c < cols) *reinterpret_cast<uint4*>(dst + r * pitch + c) = v;
+    }
+    __syncwarp();
+}
+
 // ---- the kernel ---------------------------------------------------------------
 
 struct Shared {
@@ -231,7 +253,7 @@ template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { retu
 // Five stages where the epilogue needs its patches, six where it works on whole rows.
 template <class Epi> __host__ __device__ constexpr int stage_count() { return Epi::kWholeRow ? kMaxStages : kMaxStages - 1; }
 template <int CG, int BN, class Epi> __host__ __device__ constexpr int smem_bytes() {
-    return stage_count<Epi>() * stage_bytes<CG, BN>() + (Epi::kWholeRow ? 0 : kPatchBytes) + 1024;
+    return stage_count<Epi>() * stage_bytes<CG, BN>() + (Epi::kWholeRow ? kRowPatchBytes : kPatchBytes) + 1024;
 }
 
 // The mirror image of a 32 x 32 patch whose values the warp holds as v: 8 columns at (lane % 4) * 8 of rows lane / 4 + 8 i.
@@ -451,11 +473,11 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
                 break;
             }
             tc_fence_after();
+            uint8_t* patches = smem_raw + (base - smem_u32(smem_raw)) + kStages * kStage;
             if constexpr (Epi::kWholeRow) {
-                epi.template row<BN / 2>(lanes + acc * BN, row + lane, col);
+                epi.template row<BN / 2>(lanes + acc * BN, row, lane, col, patches + (warp - 4) * 32 * kRowPatch);
             } else {
-                float* patch = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + kStages * kStage) +
-                               (warp - 4) * 32 * kPatchPitch;
+                float* patch = reinterpret_cast<float*>(patches) + (warp - 4) * 32 * kPatchPitch;
                 epilogue_by_patch<BN / 2>(epi, ops, patch, lanes + acc * BN, lane, tile.batch, row, col,
                                           p.half && tile.tm != tile.tn);
             }
@@ -561,7 +583,7 @@ struct Problem {
     bool sym;               // A A^T: half of the tiles suffices
 };
 struct Shape {
-    bool pairs;
+    int cg, bn;             // 2, 256: tiles of CTA pairs; 1, 128; 1, 64
     int slices;
     bool half;              // compute the tiles on and above the diagonal only and mirror them
 };
@@ -628,7 +650,9 @@ ac_status launch_one(const Operand& a, const Operand& b, const Problem& q, const
 
 template <bool AMN, bool BMN, class Epi>
 ac_status launch_shaped(const Operand& a, const Operand& b, const Problem& q, const Shape& s, Call& call, const Epi& epi) {
-    return s.pairs ? launch_one<2, 256, AMN, BMN>(a, b, q, s, call, epi) : launch_one<1, 128, AMN, BMN>(a, b, q, s, call, epi);
+    if (s.cg == 2) return launch_one<2, 256, AMN, BMN>(a, b, q, s, call, epi);
+    if (s.bn == 64) return launch_one<1, 64, AMN, BMN>(a, b, q, s, call, epi);
+    return launch_one<1, 128, AMN, BMN>(a, b, q, s, call, epi);
 }
 
 // D = A B^T for operands of one layout pair.
@@ -641,7 +665,7 @@ ac_status launch(const Operand& a, const Operand& b, const Problem& q, Call& cal
             const SliceEpi slice{static_cast<float*>(call.scratch), q.m, pitch};
             const ac_status rc = launch_shaped<AMN, BMN>(a, b, q, s, call, slice);
             if (rc != AC_OK) return rc;
-            const SliceSums sums{slice.out, q.m, pitch, s.slices, q.batch, s.half ? (s.pairs ? 256 : 128) : 0};
+            const SliceSums sums{slice.out, q.m, pitch, s.slices, q.batch, s.half ? s.bn : 0};
             const long long patches = (long long)((q.m + 31) / 32) * ((pitch + 31) / 32);
             AC_CUDA_TRY(launch_after(join_slices_kernel<Epi>, dim3((unsigned)((patches + 7) / 8), 1, q.batch), dim3(256), 0,
                                      call.stream, sums, epi));

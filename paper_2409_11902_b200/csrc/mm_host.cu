@@ -43,12 +43,12 @@ ac_status make_map(CUtensorMap* map, const Operand& o, bool bf16, int tile_rows)
 
 Params make_params(const Problem& q, const Shape& s, bool a_mn, bool b_mn) {
     Params p{};
-    const int cg = s.pairs ? 2 : 1, edge = 128 * cg;      // tiles are square
+    const int edge = 128 * s.cg;
     p.m = q.m;
     p.n = q.n;
     p.ktiles = ceil_div(q.k, kBK);
     p.tiles_m = ceil_div(q.m, edge);
-    p.tiles_n = ceil_div(q.n, edge);
+    p.tiles_n = ceil_div(q.n, s.bn);
     p.half = s.half;
     p.same = q.sym;
     p.batch = q.batch;
@@ -58,14 +58,14 @@ Params make_params(const Problem& q, const Shape& s, bool a_mn, bool b_mn) {
     // The smaller operand is cycled through while the larger one streams past once, as far as the panels of the
     // smaller one fit a third of the L2 (126 MB); at least 8 tiles, so that the tiles in flight stay squarish.
     p.fast_m = q.m <= q.n;
-    const long long panel = edge * q.k * 2 / s.slices;
+    const long long panel = (p.fast_m ? edge : s.bn) * q.k * 2 / s.slices;
     const long long g = (40ll << 20) / (panel > 0 ? panel : 1);
     const int tf = p.fast_m ? p.tiles_m : p.tiles_n;
     p.group = (int)(g < 8 ? 8 : g < tf ? g : tf);
     if (p.group > tf) p.group = tf;
     const uint32_t type = q.bf16 ? 1u : 0u;
     p.idesc = (1u << 4) | (type << 7) | (type << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-              ((uint32_t)(edge >> 3) << 17) | ((uint32_t)(edge >> 4) << 24);
+              ((uint32_t)(s.bn >> 3) << 17) | ((uint32_t)(edge >> 4) << 24);
     return p;
 }
 
@@ -73,27 +73,29 @@ size_t slice_bytes(const Problem& q, int slices) {
     return (size_t)slices * q.batch * q.m * ((q.n + 7) / 8 * 8) * 4;
 }
 
-// Expected time in us, from measured rates: a K-tile takes an SM 0.27 us in either shape; the epilogue of a tile 2 us of
-// a lone CTA and 4 us of a pair, twice that where it is mirrored, hidden behind the next tile's products where there is
-// one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s).
+// Expected time in us, from measured rates: a K-tile takes an SM 0.27 us, 0.20 us with 64 columns; the epilogue of a tile
+// 4 us of a pair, 2 us of a lone CTA, 1.2 us with 64 columns, twice that where it is mirrored, hidden behind the next tile's
+// products where there is one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s).
 Shape shape(const Problem& q, bool whole_row, size_t scratch) {
-    Shape best{false, 1, false};
+    Shape best{1, 128, 1, false};
     double least = 1e30;
     const int ktiles = ceil_div(q.k, kBK);
-    for (int pairs = 0; pairs < 2; ++pairs) {
-        const int edge = pairs ? 256 : 128, units = pairs ? kNumSMs / 2 : kNumSMs;
-        const long long tm = ceil_div(q.m, edge), tn = ceil_div(q.n, edge);
+    const struct { int cg, bn; double ktile, tail; } kinds[] = {{1, 128, 0.27, 2.0}, {2, 256, 0.27, 4.0}, {1, 64, 0.20, 1.2}};
+    for (const auto& kind : kinds) {
+        if (q.sym && kind.bn == 64) continue;        // diagonal tiles have to be square
+        const int units = kNumSMs / kind.cg;
+        const long long tm = ceil_div(q.m, 128 * kind.cg), tn = ceil_div(q.n, kind.bn);
         for (int half = 0; half <= (q.sym ? 1 : 0); ++half) {
             const long long tiles = (half ? tn * (tn + 1) / 2 : tm * tn) * q.batch;
-            const double tail = (pairs ? 4.0 : 2.0) * (half ? 2 : 1);
+            const double tail = kind.tail * (half ? 2 : 1);
             for (int s = 1; s <= (whole_row ? 1 : kMaxSlices) && (s == 1 || s * 2 <= ktiles); ++s) {
                 if (s > 1 && slice_bytes(q, s) > scratch) break;
-                const double waves = (double)((tiles * s + units - 1) / units), main = (double)ktiles / s * 0.27;
+                const double waves = (double)((tiles * s + units - 1) / units), main = (double)ktiles / s * kind.ktile;
                 double t = waves * (main > tail ? main : tail) + (main > tail ? tail : main);
                 if (s > 1) t += 6.0 + (double)slice_bytes(q, s) * 2 / 5e6;
                 if (t < least * 0.97) {      // the simpler one unless the other is worth it
                     least = t;
-                    best = Shape{pairs != 0, s, half != 0};
+                    best = Shape{kind.cg, kind.bn, s, half != 0};
                 }
             }
         }
