@@ -166,19 +166,23 @@ struct GradEpi : Ce {
 
 // A gradient: bf16 to the caller's dense matrix and/or fp32 sums over the pieces.
 struct OutEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kScalar = true;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true;
     __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
     float* sum;             // [rows][pitch], or null
     const float* top;       // what g was divided by
     int add;                // 1: what earlier pieces left in `sum` is added
     int rows, cols, pitch;
-    __device__ __forceinline__ bool scalar() const { return out && cols % 8 != 0; }
-    __device__ __forceinline__ void store1(int, int row, int col, float v) const {
-        if (row < rows && col < cols) out[(long long)row * cols + col] = __float2bfloat16(v);
+    __device__ __forceinline__ bool ragged() const { return out && cols % 8 != 0; }
+    __device__ __forceinline__ void store_ragged_patch(float* patch, int lane, int, int row, int col, const float (&v)[4][8]) const {
+        store_ragged(out, 0, rows, cols, patch, lane, row, col, v);
     }
-    template <int R> struct Ops { float4 x[R][2]; };
+    template <int R> struct Ops {
+        float4 x[R][2];
+        float scale;
+    };
     template <int R>
     __device__ __forceinline__ void load(Ops<R>& o, int, int row, int step, int col) const {
+        o.scale = *top;
         if (!add || col >= cols) return;
 #pragma unroll
         for (int i = 0; i < R; ++i)
@@ -200,9 +204,8 @@ struct OutEpi {
                 v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
             }
             if (out) {
-                const float scale = *top;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] *= scale;
+                for (int j = 0; j < 8; ++j) v[i][j] *= o.scale;
                 if (cols % 8 == 0) store8(out + (long long)row * cols + col, v[i]);
             } else {
                 float4* q = reinterpret_cast<float4*>(sum + (long long)row * pitch + col);

@@ -6,8 +6,8 @@
 // accumulators is the epilogue's business: a functor gets them 8 consecutive columns of a row at a time,
 // or reads a row's half tile from tensor memory itself (kWholeRow).
 //
-// One CTA per SM, 12 warps: warp 0 loads K-tiles of 64 by TMA into a ring of shared-memory stages (128-byte swizzle),
-// warp 1 issues the MMAs, warp 2 owns the tensor memory, warps 4-11 run the epilogue of one accumulator while the
+// One CTA per SM, 12 warps: warps 0 and 3 load K-tiles of 64 by TMA into a ring of shared-memory stages (128-byte
+// swizzle), warp 1 issues the MMAs, warp 2 owns the tensor memory, warps 4-11 run the epilogue of one accumulator while the
 // other one is being filled (two accumulators of BN columns). Two shapes:
 //   CG = 2, BN = 256: a pair of SMs computes a 256 x 256 tile (cta_group::2); each holds 128 rows of A and 128 rows
 //           of B, so a K-tile costs 32 KB of shared memory per SM for twice the MMA work of a lone 128 x 128 tile.
@@ -34,9 +34,9 @@ using namespace tc;
 constexpr int kThreads = 384;
 constexpr int kEpiWarps = 8;
 constexpr int kBK = 64;                      // K-tile: one 128-byte swizzle row of 16-bit elements
-constexpr int kMaxStages = 6;
-constexpr int kPatchPitch = 36;              // floats between the rows of a warp's 32 x 32 patch: no bank conflicts
-constexpr int kPatchBytes = kEpiWarps * 32 * kPatchPitch * 4;
+constexpr int kMaxStages = 8;
+constexpr int kPatch = 32 * 32;              // floats of a warp's patch
+constexpr int kPatchBytes = kEpiWarps * kPatch * 4;
 constexpr int kRowPatch = 80;                // bytes between the rows of a warp's 32 x 32 patch of 16-bit values
 constexpr int kRowPatchBytes = kEpiWarps * 32 * kRowPatch;
 constexpr int kMaxSlices = 16;
@@ -250,76 +250,90 @@ __device__ __forceinline__ void flag_timeout(int* abort_s, uint32_t* status, uin
 }
 
 template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { return 128 * 128 + BN / CG * 128; }
-// Five stages where the epilogue needs its patches, six where it works on whole rows.
-template <class Epi> __host__ __device__ constexpr int stage_count() { return Epi::kWholeRow ? kMaxStages : kMaxStages - 1; }
+// As many stages as fit (six, eight with 64 columns): the L2 answers a load after about 1.1 us, so the bytes in flight set
+// the rate at which K-tiles arrive.
+template <int CG, int BN> __host__ __device__ constexpr int stage_count() { return 6 * 32768 / stage_bytes<CG, BN>(); }
 template <int CG, int BN, class Epi> __host__ __device__ constexpr int smem_bytes() {
-    return stage_count<Epi>() * stage_bytes<CG, BN>() + (Epi::kWholeRow ? kRowPatchBytes : kPatchBytes) + 1024;
+    return stage_count<CG, BN>() * stage_bytes<CG, BN>() + (Epi::kWholeRow ? kRowPatchBytes : kPatchBytes) + 1024;
 }
 
-// The mirror image of a 32 x 32 patch whose values the warp holds as v: 8 columns at (lane % 4) * 8 of rows lane / 4 + 8 i.
+// Tensor memory gives a thread one row; memory wants the threads of a warp side by side along rows. A warp passes 32 x 32
+// values through a patch of shared memory, after which 4 threads hold 8 columns each of one row (rows lane / 4 + 8 i, columns
+// (lane % 4) * 8): accesses of 64 bytes (16-bit results) on 8 rows at a time. The 16-byte groups of a row are permuted by the
+// row's number, so that neither direction meets bank conflicts.
+__device__ __forceinline__ float* patch_at(float* patch, int row, int group) { return patch + row * 32 + ((group ^ (row & 7)) << 2); }
+
+__device__ __forceinline__ void patch_put(float* patch, int lane, const float (&v)[4][8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + (lane >> 2), g = (lane & 3) * 2;
+        *reinterpret_cast<float4*>(patch_at(patch, r, g)) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+        *reinterpret_cast<float4*>(patch_at(patch, r, g + 1)) = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+    }
+}
+// The mirror image of the patch whose values the warp holds as v.
 template <class Epi>
 __device__ __forceinline__ void store_mirror_patch(const Epi& epi, float* patch, int lane, int batch, int row, int col,
                                                    const float (&v)[4][8]) {
     const int pr = lane >> 2, pc = (lane & 3) * 8;
     __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float* q = patch + (i * 8 + pr) * kPatchPitch + pc;
-        *reinterpret_cast<float4*>(q) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
-        *reinterpret_cast<float4*>(q + 4) = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
-    }
+    patch_put(patch, lane, v);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = patch[(pc + j) * kPatchPitch + i * 8 + pr];
+        for (int j = 0; j < 8; ++j) w[j] = patch_at(patch, pc + j, i * 2 + (pr >> 2))[pr & 3];
         epi.store_mirror(batch, col + i * 8 + pr, row + pc, w);
     }
 }
-
-// The same values to rows that no 16-byte access fits (a destination with an odd number of columns): one row at a time,
-// the 32 threads side by side.
-template <class Epi>
-__device__ __forceinline__ void store_scalar_patch(const Epi& epi, float* patch, int lane, int batch, int row, int col,
-                                                   const float (&v)[4][8]) {
-    const int pr = lane >> 2, pc = (lane & 3) * 8;
+// The same values to a dense bf16 matrix that no 16-byte access fits (its number of columns is no multiple of 8): 16 threads
+// per row, 4 bytes each, shifted by one column on rows that start at an odd element.
+__device__ __forceinline__ void store_ragged(__nv_bfloat16* out, long long base, int rows, int cols, float* patch, int lane, int row,
+                                             int col, const float (&v)[4][8]) {
     __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float* q = patch + (i * 8 + pr) * kPatchPitch + pc;
-        *reinterpret_cast<float4*>(q) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
-        *reinterpret_cast<float4*>(q + 4) = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+    patch_put(patch, lane, v);
+    __syncwarp();
+    const int l = lane & 15;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int r = i * 2 + (lane >> 4);
+        const long long at = base + (long long)(row + r) * cols + col;
+        const int odd = (int)(at & 1), c = 2 * l + odd;
+        const float x = patch_at(patch, r, c >> 2)[c & 3], y = patch_at(patch, r, ((c + 1) & 31) >> 2)[(c + 1) & 3];
+        if (row + r >= rows || col >= cols) continue;
+        if (c + 1 < 32 && col + c + 1 < cols) {
+            *reinterpret_cast<uint32_t*>(out + at + c) = pack2<__nv_bfloat16>(x, y);
+        } else if (col + c < cols) {
+            out[at + c] = __float2bfloat16(x);
+        }
+        if (odd && l == 0) out[at] = __float2bfloat16(*patch_at(patch, r, 0));
     }
-    __syncwarp();
-#pragma unroll 8
-    for (int r = 0; r < 32; ++r) epi.store1(batch, row + r, col + lane, patch[r * kPatchPitch + lane]);
 }
 
-// Tensor memory gives a thread one row; memory wants the threads of a warp side by side along rows. A warp passes 32 x 32
-// values through a patch of shared memory, after which 4 threads hold 8 columns each of one row: accesses of 64 bytes
-// (16-bit results) on 8 rows at a time. A symmetric result's mirror image is read from the patch by columns. What the
-// functor reads beside the accumulators (`ops`) is requested a patch ahead; the first before the accumulators are waited for.
+// What the functor reads beside the accumulators (`ops`) is requested a patch ahead, the first before the accumulators are
+// waited for.
 template <int COLS, class Epi>
 __device__ __forceinline__ void epilogue_by_patch(const Epi& epi, typename Epi::template Ops<4>& ops, float* patch, uint32_t taddr,
                                                   int lane, int batch, int row, int col, bool mirror) {
     const int pr = lane >> 2, pc = (lane & 3) * 8;
+    uint32_t r[32];
+    tmem_ld32_issue(taddr, r);
 #pragma unroll 2
     for (int c = 0; c < COLS; c += 32) {
-        uint32_t r[32];
-        tmem_ld32(taddr + c, r);
-        float* own = patch + lane * kPatchPitch;
+        tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 32; j += 4)
-            *reinterpret_cast<uint4*>(own + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+        for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(patch_at(patch, lane, j)) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
         __syncwarp();
+        if (c + 32 < COLS) tmem_ld32_issue(taddr + c + 32, r);
         typename Epi::template Ops<4> now = ops;
         if (c + 32 < COLS) epi.load(ops, batch, row + pr, 8, col + c + 32 + pc);
         float v[4][8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float* q = patch + (i * 8 + pr) * kPatchPitch + pc;
-            const float4 a = *reinterpret_cast<const float4*>(q), b = *reinterpret_cast<const float4*>(q + 4);
+            const float4 a = *reinterpret_cast<const float4*>(patch_at(patch, i * 8 + pr, (lane & 3) * 2));
+            const float4 b = *reinterpret_cast<const float4*>(patch_at(patch, i * 8 + pr, (lane & 3) * 2 + 1));
             v[i][0] = a.x; v[i][1] = a.y; v[i][2] = a.z; v[i][3] = a.w;
             v[i][4] = b.x; v[i][5] = b.y; v[i][6] = b.z; v[i][7] = b.w;
         }
@@ -327,8 +341,8 @@ __device__ __forceinline__ void epilogue_by_patch(const Epi& epi, typename Epi::
         if constexpr (Epi::kMirror) {
             if (mirror) store_mirror_patch(epi, patch, lane, batch, row, col + c, v);
         }
-        if constexpr (Epi::kScalar) {
-            if (epi.scalar()) store_scalar_patch(epi, patch, lane, batch, row, col + c, v);
+        if constexpr (Epi::kRagged) {
+            if (epi.ragged()) epi.store_ragged_patch(patch, lane, batch, row, col + c, v);
         }
         __syncwarp();
     }
@@ -340,7 +354,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
           const __grid_constant__ Params p, const __grid_constant__ Epi epi) {
     constexpr int NB = BN / CG;               // rows of B that one CTA holds
     constexpr uint32_t kStage = stage_bytes<CG, BN>();
-    constexpr int kStages = stage_count<Epi>();
+    constexpr int kStages = stage_count<CG, BN>();
     extern __shared__ uint8_t smem_raw[];
     __shared__ Shared sh;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -351,7 +365,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
 
     if (tid == 0) {
         sh.abort = 0;
-        for (int s = 0; s < kMaxStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int s = 0; s < kMaxStages; ++s) { mbar_init(&sh.full[s], 2); mbar_init(&sh.empty[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&sh.tfull[a], 1); mbar_init(&sh.tempty[a], kEpiWarps * CG); }
         fence_barrier_init();
         prefetch_tmap(&ta);
@@ -364,24 +378,28 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     pdl_launch_dependents();
-    if (p.reset_status && blockIdx.x == 0 && tid == 96) {
+    if (p.reset_status && blockIdx.x == 0 && tid == 64) {
         pdl_wait();
         p.status[0] = 0u;
         p.status[1] = 0u;
     }
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
         // ---------------------------------------------------------------- loads
+        // Warp 0 loads A, warp 3 loads B: issuing a tensor copy holds a warp for some hundred cycles, and one warp for both
+        // operands made K-tiles no faster than one per 0.27 us however small they were.
         if (elect_one()) {
+            const bool is_a = warp == 0;
+            const void* map = is_a ? &ta : &tb;
+            constexpr uint32_t kBytesA = 128 * 128, kBytesB = NB * 128;
             int it = 0;
             bool ok = true;
             Tile tile = decode_tile(p, unit);
             pdl_wait();
             for (int t = unit; t < p.tiles && ok; t += units) {
                 if (t != unit) tile = decode_tile(p, t);
-                const int row0 = tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0);
-                const int col0 = tile.tn * BN + (CG == 2 ? (int)rank * NB : 0);
-                const bool once = p.same && tile.tm == tile.tn;
+                const int at = is_a ? tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) : tile.tn * BN + (CG == 2 ? (int)rank * NB : 0);
+                const bool skip = !is_a && p.same && tile.tm == tile.tn;      // B's rows are A's
                 const int matrix = tile.batch % p.batch;
                 for (int kt = tile.k0; kt < tile.k1; ++kt, ++it) {
                     const int s = it % kStages;
@@ -391,24 +409,23 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
                         break;
                     }
                     // a pair's loads all complete on the leader's barrier; it alone announces the bytes of both
-                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&sh.full[s], (once ? 128 * 128 : kStage) * CG);
+                    if (CG == 1 || rank == 0) {
+                        if (skip)
+                            mbar_arrive(&sh.full[s]);
+                        else
+                            mbar_arrive_expect_tx(&sh.full[s], (is_a ? kBytesA : kBytesB) * CG);
+                    }
+                    if (skip) continue;
                     uint32_t bar = smem_u32(&sh.full[s]);
                     if constexpr (CG == 2) bar = map_rank(bar, 0);
-                    const uint32_t a = base + s * kStage, b = a + 128 * 128;
-                    if constexpr (AMN) {
+                    const uint32_t to = base + s * kStage + (is_a ? 0 : kBytesA);
+                    const int slabs = is_a ? (AMN ? 2 : 0) : (BMN ? NB / 64 : 0);
+                    if (slabs == 0) {
+                        tma_load_3d<CG>(to, map, bar, kt * kBK, at, matrix);
+                    } else {
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
-                            tma_load_3d<CG>(a + j * 8192, &ta, bar, row0 + 64 * j, kt * kBK, matrix);
-                    } else {
-                        tma_load_3d<CG>(a, &ta, bar, kt * kBK, row0, matrix);
-                    }
-                    if (once) continue;
-                    if constexpr (BMN) {
-#pragma unroll
-                        for (int j = 0; j < NB / 64; ++j)
-                            tma_load_3d<CG>(b + j * 8192, &tb, bar, col0 + 64 * j, kt * kBK, matrix);
-                    } else {
-                        tma_load_3d<CG>(b, &tb, bar, kt * kBK, col0, matrix);
+                            if (j < slabs) tma_load_3d<CG>(to + j * 8192, map, bar, at + 64 * j, kt * kBK, matrix);
                     }
                 }
             }
@@ -477,7 +494,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             if constexpr (Epi::kWholeRow) {
                 epi.template row<BN / 2>(lanes + acc * BN, row, lane, col, patches + (warp - 4) * 32 * kRowPatch);
             } else {
-                float* patch = reinterpret_cast<float*>(patches) + (warp - 4) * 32 * kPatchPitch;
+                float* patch = reinterpret_cast<float*>(patches) + (warp - 4) * kPatch;
                 epilogue_by_patch<BN / 2>(epi, ops, patch, lanes + acc * BN, lane, tile.batch, row, col,
                                           p.half && tile.tm != tile.tn);
             }
@@ -509,7 +526,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
 
 // The sums of one slice, fp32, in the workspace: [slice][batch][rows][pitch].
 struct SliceEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kScalar = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false;
     float* out;
     int rows, pitch;
     template <int R> struct Ops {};
@@ -536,7 +553,7 @@ struct SliceSums {
 // Adds the slices, first to last, and applies the epilogue. A warp per 32 x 32 patch, grid (patches / 8, 1, batch).
 template <class Epi>
 __global__ void __launch_bounds__(256) join_slices_kernel(const __grid_constant__ SliceSums p, const __grid_constant__ Epi epi) {
-    __shared__ __align__(16) float patches[Epi::kMirror || Epi::kScalar ? kEpiWarps * 32 * kPatchPitch : 4];
+    __shared__ __align__(16) float patches[Epi::kMirror || Epi::kRagged ? kEpiWarps * kPatch : 4];
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, across = (p.pitch + 31) / 32;
@@ -547,28 +564,29 @@ __global__ void __launch_bounds__(256) join_slices_kernel(const __grid_constant_
     typename Epi::template Ops<4> ops;
     epi.load(ops, batch, r, 8, c);
     float v[4][8] = {};
-    if (c < p.pitch) {
-        const long long stride = (long long)p.batch * p.rows * p.pitch;
-        const float* from = p.in + ((long long)batch * p.rows + r) * p.pitch + c;
-#pragma unroll 2
-        for (int s = 0; s < p.slices; ++s, from += stride) {
+    // rows clamped, not guarded: a guard around load and addition would make the loads wait for one another
+    const long long stride = (long long)p.batch * p.rows * p.pitch;
+    const float* from[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (r + i * 8 >= p.rows) continue;
-                const float4 a = *reinterpret_cast<const float4*>(from + (long long)i * 8 * p.pitch);
-                const float4 b = *reinterpret_cast<const float4*>(from + (long long)i * 8 * p.pitch + 4);
-                v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
-                v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
-            }
+    for (int i = 0; i < 4; ++i)
+        from[i] = p.in + ((long long)batch * p.rows + min(r + i * 8, p.rows - 1)) * p.pitch + min(c, p.pitch - 8);
+#pragma unroll 4
+    for (int s = 0; s < p.slices; ++s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 a = *reinterpret_cast<const float4*>(from[i] + s * stride);
+            const float4 b = *reinterpret_cast<const float4*>(from[i] + s * stride + 4);
+            v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
+            v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
         }
     }
     epi.apply(ops, batch, r, 8, c, v);
     if constexpr (Epi::kMirror) {
         if (p.sym && col / p.sym != row / p.sym)
-            store_mirror_patch(epi, patches + warp * 32 * kPatchPitch, lane, batch, row, col, v);
+            store_mirror_patch(epi, patches + warp * kPatch, lane, batch, row, col, v);
     }
-    if constexpr (Epi::kScalar) {
-        if (epi.scalar()) store_scalar_patch(epi, patches + warp * 32 * kPatchPitch, lane, batch, row, col, v);
+    if constexpr (Epi::kRagged) {
+        if (epi.ragged()) epi.store_ragged_patch(patches + warp * kPatch, lane, batch, row, col, v);
     }
 }
 
