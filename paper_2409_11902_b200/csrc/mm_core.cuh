@@ -432,44 +432,39 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         }
     } else if (warp == 1 && (CG == 1 || rank == 0)) {
         // ----------------------------------------------------------------- MMAs
-        // The whole warp runs the loop, so that the descriptor arithmetic stays in uniform registers.
-        const bool leader = elect_one();
-        const uint32_t hi = desc_hi(1024, 2);
-        int it = 0, n = 0;
-        bool ok = true;
-        for (int t = unit; t < p.tiles && ok; t += units, ++n) {
-            const int acc = n & 1;
-            bool got = mbar_wait(&sh.tempty[acc], ((n >> 1) & 1) ^ 1, abort_flag);
-            if (!__all_sync(0xffffffffu, got)) {
-                if (leader) flag_timeout(&sh.abort, p.status, 0x1200u + acc);
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            const uint32_t d = tmem + acc * BN;
-            const Tile tile = decode_tile(p, t);
-            const uint32_t b_off = p.same && tile.tm == tile.tn ? 0 : 128 * 128;
-            for (int kt = tile.k0; kt < tile.k1; ++kt, ++it) {
-                const int s = it % kStages;
-                got = mbar_wait(&sh.full[s], (it / kStages) & 1, abort_flag);
-                if (!__all_sync(0xffffffffu, got)) {
-                    if (leader) flag_timeout(&sh.abort, p.status, 0x1300u + s);
-                    ok = false;
+        // One thread: 32 that poll a barrier side by side take its turns from the loading warps.
+        if (elect_one()) {
+            const uint32_t hi = desc_hi(1024, 2);
+            int it = 0, n = 0;
+            bool ok = true;
+            for (int t = unit; t < p.tiles && ok; t += units, ++n) {
+                const int acc = n & 1;
+                const Tile tile = decode_tile(p, t);
+                if (!mbar_wait(&sh.tempty[acc], ((n >> 1) & 1) ^ 1, abort_flag)) {
+                    flag_timeout(&sh.abort, p.status, 0x1200u + acc);
                     break;
                 }
                 tc_fence_after();
-                const uint32_t a_lo = desc_lo(base + s * kStage, AMN ? 8192 : 16);
-                const uint32_t b_lo = desc_lo(base + s * kStage + b_off, BMN ? 8192 : 16);
+                const uint32_t d = tmem + acc * BN;
+                const uint32_t b_off = p.same && tile.tm == tile.tn ? 0 : 128 * 128;
+                for (int kt = tile.k0; kt < tile.k1; ++kt, ++it) {
+                    const int s = it % kStages;
+                    if (!mbar_wait(&sh.full[s], (it / kStages) & 1, abort_flag)) {
+                        flag_timeout(&sh.abort, p.status, 0x1300u + s);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a_lo = desc_lo(base + s * kStage, AMN ? 8192 : 16);
+                    const uint32_t b_lo = desc_lo(base + s * kStage + b_off, BMN ? 8192 : 16);
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk)     // K = 16 each: 32 bytes along a K-major row, 16 rows of an MN-major slab
-                    if (leader)
+                    for (int kk = 0; kk < 4; ++kk)     // K = 16 each: 32 bytes along a K-major row, 16 rows of an MN-major slab
                         mma_words<CG>(d, a_lo + kk * (AMN ? 128 : 2), hi, b_lo + kk * (BMN ? 128 : 2), hi, p.idesc,
                                       (uint32_t)(kt > tile.k0 || kk > 0));
-                if (leader) commit_cg<CG>(&sh.empty[s]);
-                __syncwarp();
+                    commit_cg<CG>(&sh.empty[s]);
+                }
+                if (ok) commit_cg<CG>(&sh.tfull[acc]);
             }
-            if (ok && leader) commit_cg<CG>(&sh.tfull[acc]);
-            __syncwarp();
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------- epilogue
@@ -484,8 +479,9 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             const int col = tile.tn * BN + half * (BN / 2);
             typename Epi::template Ops<4> ops;
             epi.load(ops, tile.batch, row + (lane >> 2), 8, col + (lane & 3) * 8);
-            const bool got = mbar_wait(&sh.tfull[acc], (n >> 1) & 1, abort_flag);
-            if (!__all_sync(0xffffffffu, got)) {
+            bool got = true;
+            if (lane == 0) got = mbar_wait(&sh.tfull[acc], (n >> 1) & 1, abort_flag);
+            if (!__shfl_sync(0xffffffffu, (int)got, 0)) {
                 if (lane == 0) flag_timeout(&sh.abort, p.status, 0x1400u + acc);
                 break;
             }
