@@ -15,8 +15,8 @@
 // Where the tiles are too few and K is long, K is cut into slices: each is a tile of its own that leaves fp32 sums in the
 // workspace, and a second kernel adds the slices in their order and applies the epilogue (a cluster that adds them up in
 // distributed shared memory was slower: that memory gives about 25 GB/s to an SM, the L2 three times as much).
-// A K-tile of 64 takes an SM 0.27 us in the first two shapes (64 bytes per clock from the L2, or the MMAs of a pair) and
-// 0.20 us in the last; shape() chooses shape and slices by these rates.
+// A K-tile of 64 takes an SM 0.27 us in the first shape (its MMAs) and about 0.2 us in the other two; shape() chooses
+// shape and slices by these rates.
 #pragma once
 
 #include <cuda.h>
@@ -288,27 +288,48 @@ __device__ __forceinline__ void store_mirror_patch(const Epi& epi, float* patch,
     }
 }
 // The same values to a dense bf16 matrix that no 16-byte access fits (its number of columns is no multiple of 8): 16 threads
-// per row, 4 bytes each, shifted by one column on rows that start at an odd element.
+// per row, 4 bytes each, shifted by one column on rows that start at an odd element, whose first and last column follow by
+// themselves. The patch that ends past the last column is stored element by element.
 __device__ __forceinline__ void store_ragged(__nv_bfloat16* out, long long base, int rows, int cols, float* patch, int lane, int row,
                                              int col, const float (&v)[4][8]) {
     __syncwarp();
     patch_put(patch, lane, v);
     __syncwarp();
-    const int l = lane & 15;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int r = i * 2 + (lane >> 4);
-        const long long at = base + (long long)(row + r) * cols + col;
-        const int odd = (int)(at & 1), c = 2 * l + odd;
-        const float x = patch_at(patch, r, c >> 2)[c & 3], y = patch_at(patch, r, ((c + 1) & 31) >> 2)[(c + 1) & 3];
-        if (row + r >= rows || col >= cols) continue;
-        if (c + 1 < 32 && col + c + 1 < cols) {
-            *reinterpret_cast<uint32_t*>(out + at + c) = pack2<__nv_bfloat16>(x, y);
-        } else if (col + c < cols) {
-            out[at + c] = __float2bfloat16(x);
+    const long long first = base + (long long)row * cols + col;
+    const int left = rows - row;
+    if (col + 32 <= cols) {
+        const int l = lane & 15, r0 = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            float x[8], y[8];
+            long long at[8];
+            int c[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = (i + j) * 2 + r0;
+                at[j] = first + (long long)r * cols;
+                c[j] = 2 * l + (int)(at[j] & 1);
+                x[j] = patch_at(patch, r, c[j] >> 2)[c[j] & 3];
+                y[j] = patch_at(patch, r, ((c[j] + 1) & 31) >> 2)[(c[j] + 1) & 3];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if ((i + j) * 2 + r0 < left && c[j] < 31) *reinterpret_cast<uint32_t*>(out + at[j] + c[j]) = pack2<__nv_bfloat16>(x[j], y[j]);
         }
-        if (odd && l == 0) out[at] = __float2bfloat16(*patch_at(patch, r, 0));
+        const long long at = first + (long long)lane * cols;
+        const float x = *patch_at(patch, lane, 0), y = patch_at(patch, lane, 7)[3];
+        if (lane < left && (at & 1)) {
+            out[at] = __float2bfloat16(x);
+            out[at + 31] = __float2bfloat16(y);
+        }
+    } else if (col + lane < cols) {
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) {
+            const float x = patch_at(patch, r, lane >> 2)[lane & 3];
+            if (r < left) out[first + (long long)r * cols + lane] = __float2bfloat16(x);
+        }
     }
+    __syncwarp();
 }
 
 // What the functor reads beside the accumulators (`ops`) is requested a patch ahead, the first before the accumulators are

@@ -73,14 +73,14 @@ size_t slice_bytes(const Problem& q, int slices) {
     return (size_t)slices * q.batch * q.m * ((q.n + 7) / 8 * 8) * 4;
 }
 
-// Expected time in us, from measured rates: a K-tile takes an SM 0.27 us, 0.20 us with 64 columns; the epilogue of a tile
+// Expected time in us, from measured rates: a K-tile takes a pair 0.27 us, a lone CTA 0.21 us, 0.19 us with 64 columns; the epilogue of a tile
 // 4 us of a pair, 2 us of a lone CTA, 1.2 us with 64 columns, twice that where it is mirrored, hidden behind the next tile's
 // products where there is one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s).
 Shape shape(const Problem& q, bool whole_row, size_t scratch) {
     Shape best{1, 128, 1, false};
     double least = 1e30;
     const int ktiles = ceil_div(q.k, kBK);
-    const struct { int cg, bn; double ktile, tail; } kinds[] = {{1, 128, 0.27, 2.0}, {2, 256, 0.27, 4.0}, {1, 64, 0.20, 1.2}};
+    const struct { int cg, bn; double ktile, tail; } kinds[] = {{1, 128, 0.21, 2.0}, {2, 256, 0.27, 4.0}, {1, 64, 0.19, 1.1}};
     for (const auto& kind : kinds) {
         if (q.sym && kind.bn == 64) continue;        // diagonal tiles have to be square
         const int units = kNumSMs / kind.cg;
