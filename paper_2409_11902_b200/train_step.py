@@ -20,6 +20,11 @@ Only the two `ac_*` calls are this library's kernels; convolution forward, input
 norm, pooling, the classifier, the loss and the optimizer are the framework's. bf16 activations in
 channels-last memory, fp32 master weights, SGD with momentum. No dataset: images ~ N(0,1), labels
 uniform over 1000 classes, weights randomly initialised.
+
+Two more parts of the step can be the library's (`head="fused"`, `optimizer="muon"`): the classifier
+with its loss, whose logits are then never kept (`ac_linear_ce_step`), and the update of the
+convolutions' weights, orthogonalised from the weight gradients as they lie (`ac_muon_update`; batch
+norms and the classifier stay with SGD).
 """
 from __future__ import annotations
 
@@ -124,6 +129,71 @@ class ReluKeepingMask(torch.autograd.Function):
         return dx, None, None
 
 
+class LinearCrossEntropy(torch.autograd.Function):
+    """Mean cross entropy of the linear classifier x w^T + b over the rows with a label. The gradients of the mean are
+    formed in the forward pass (their weights, 1 / count, are known there); backward scales them."""
+
+    @staticmethod
+    def forward(ctx, x, w_master, b_master, labels):
+        x = x.to(torch.bfloat16).contiguous()
+        w = w_master.to(torch.bfloat16).contiguous()
+        b = None if b_master is None else b_master.to(torch.bfloat16).contiguous()
+        d = api.LinearCeDesc(x.shape[0], w.shape[0], x.shape[1], bias=b is not None)
+        counts = (labels >= 0) & (labels < w.shape[0])
+        dloss = counts / counts.sum().clamp(min=1)
+        loss, lse = torch.empty_like(dloss), torch.empty_like(dloss)
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), None if b is None else torch.empty_like(b)
+        ws = torch.empty(api.ac_linear_ce_workspace_bytes(d), dtype=torch.uint8, device=x.device)
+        api.ac_linear_ce_step(d, x, w, b, labels.contiguous(), dloss, loss, lse, dx, dw, db, ws)
+        ctx.grads = dx, dw, db
+        return (loss * dloss).sum()
+
+    @staticmethod
+    def backward(ctx, g):
+        dx, dw, db = ctx.grads
+        ctx.grads = None
+        return dx * g.to(dx.dtype), dw.float() * g, None if db is None else db.float() * g, None
+
+
+class Muon:
+    """Momentum and orthogonalised updates for convolution weights. Weights of one shape are updated in one call, as a batch
+    of matrices [C_out][R*S*C_in] (the order in which the compressed weight gradient is written); other parameters get plain
+    SGD with momentum. The update's entries have a root mean square of about `scale` / sqrt(longer side)."""
+
+    def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, steps=5, sgd_lr=0.1, sgd_momentum=0.9):
+        self.lr, self.groups = lr, []
+        params = list(params)
+        shapes = {}
+        for p in params:
+            if p.dim() == 4:
+                shapes.setdefault(tuple(p.shape), []).append(p)
+        for (co, ci, r, s), ps in shapes.items():
+            d = api.MuonDesc(co, r * s * ci, batch=len(ps), momentum=momentum, nesterov=nesterov, steps=steps,
+                             scale=math.sqrt(max(1.0, co / (r * s * ci))))
+            matrices = lambda dtype: torch.zeros((len(ps), co, r * s * ci), dtype=dtype, device=ps[0].device)  # noqa: E731
+            self.groups.append(dict(desc=d, params=ps, momentum=matrices(torch.float32), update=matrices(torch.bfloat16),
+                                    workspace=torch.empty(api.ac_muon_workspace_bytes(d), dtype=torch.uint8,
+                                                          device=ps[0].device)))
+        self.sgd = torch.optim.SGD([p for p in params if p.dim() != 4], lr=sgd_lr, momentum=sgd_momentum)
+
+    def zero_grad(self, set_to_none=True):
+        self.sgd.zero_grad(set_to_none=set_to_none)
+        for g in self.groups:
+            for p in g["params"]:
+                p.grad = None
+
+    @torch.no_grad()
+    def step(self):
+        for g in self.groups:
+            d, ps = g["desc"], g["params"]
+            grad = torch.stack([p.grad.permute(0, 2, 3, 1).reshape(d.rows, d.cols) for p in ps])
+            api.ac_muon_update(d, grad, g["momentum"], g["momentum"], g["update"], g["workspace"])
+            for p, u in zip(ps, g["update"]):
+                co, ci, r, s = p.shape
+                p.add_(u.view(co, r, s, ci).permute(0, 3, 1, 2), alpha=-self.lr)
+        self.sgd.step()
+
+
 class ResNet50:
     """ResNet-50 (bottleneck blocks, stride on the 3x3) as plain parameter lists; `scheme` chooses
     what the convolutions and ReLUs keep for backward."""
@@ -183,6 +253,15 @@ class ResNet50:
         return F.batch_norm(x, p["mean"], p["var"], p["w"], p["b"], True, 0.1, 1e-5)
 
     def forward(self, images):
+        return F.linear(self.features(images), self.fc_w.to(torch.bfloat16), self.fc_b.to(torch.bfloat16))
+
+    def loss(self, images, labels, head):
+        """The step's loss, its classifier and cross entropy the framework's or (head "fused") the library's."""
+        if head == "fused":
+            return LinearCrossEntropy.apply(self.features(images), self.fc_w, self.fc_b, labels)
+        return F.cross_entropy(self.forward(images).float(), labels)
+
+    def features(self, images):
         x = self.conv(images, self.stem_w, 2, 3, Saved(), compress=self.compress_stem)
         x = F.relu(self.bn(x, self.stem_bn), inplace=True)   # feeds the max pooling, which keeps it anyway
         x = F.max_pool2d(x, 3, 2, 1)
@@ -196,8 +275,7 @@ class ResNet50:
             if "wd" in blk:   # reads the same tensor as conv1: one Z for both
                 idn = self.bn(self.conv(x, blk["wd"], s, 0, saved), blk["bnd"])
             x, saved = self.relu(c + idn)
-        x = F.adaptive_avg_pool2d(x, 1).flatten(1)
-        return F.linear(x, self.fc_w.to(torch.bfloat16), self.fc_b.to(torch.bfloat16))
+        return F.adaptive_avg_pool2d(x, 1).flatten(1)
 
 
 def synthetic_batch(batch, device, seed=0, num_classes=1000):
@@ -207,7 +285,13 @@ def synthetic_batch(batch, device, seed=0, num_classes=1000):
     return images.to(device).contiguous(memory_format=torch.channels_last), labels.to(device)
 
 
-def training_step(scheme, batch=256, k=2, device="cuda", seed=0, compress_stem=True, capture=None, time_steps=0):
+def make_optimizer(name, params):
+    assert name in ("sgd", "muon")
+    return Muon(params) if name == "muon" else torch.optim.SGD(params, lr=0.1, momentum=0.9)
+
+
+def training_step(scheme, batch=256, k=2, device="cuda", seed=0, compress_stem=True, capture=None, time_steps=0,
+                  head="framework", optimizer="sgd"):
     """Runs one step and reads the allocator at Section 3's five points. Returns a dict with the
     loss and the bytes; `capture`: a list that receives (desc, X, Z, dY, dW) of every compressed
     convolution's backward (for checks; X is then copied in the forward pass, so the memory figures of such
@@ -220,12 +304,11 @@ def training_step(scheme, batch=256, k=2, device="cuda", seed=0, compress_stem=T
     mib = lambda b: (b - base) / 2.0 ** 20
     model = ResNet50(scheme, k, dev, seed, compress_stem)
     model.capture = capture
-    opt = torch.optim.SGD(model.params, lr=0.1, momentum=0.9)
+    opt = make_optimizer(optimizer, model.params)
     p1 = torch.cuda.memory_allocated(dev)
     images, labels = synthetic_batch(batch, dev, seed)
     p2 = torch.cuda.memory_allocated(dev)
-    logits = model.forward(images)
-    loss = F.cross_entropy(logits.float(), labels)
+    loss = model.loss(images, labels, head)
     torch.cuda.synchronize(dev)
     p3, p3_peak = torch.cuda.memory_allocated(dev), torch.cuda.max_memory_allocated(dev)
     torch.cuda.reset_peak_memory_stats(dev)
@@ -245,31 +328,32 @@ def training_step(scheme, batch=256, k=2, device="cuda", seed=0, compress_stem=T
     out["grad_norm"] = float(torch.sqrt(sum((p.grad.double() ** 2).sum() for p in model.params if p.grad is not None)))
     if time_steps > 0 and capture is None:
         # duration of further whole steps (forward, backward, optimizer), CUDA events on the current stream
-        del logits, loss
+        del loss
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         e0.record()
         for _ in range(time_steps):
             opt.zero_grad(set_to_none=True)
-            lg = model.forward(images)
-            ls = F.cross_entropy(lg.float(), labels)
+            ls = model.loss(images, labels, head)
             ls.backward()
             opt.step()
-            del lg, ls
+            del ls
         e1.record()
         torch.cuda.synchronize(dev)
         out["step_ms"] = e0.elapsed_time(e1) / time_steps
-        logits = loss = None
-    del model, opt, images, labels, logits, loss
+        loss = None
+    del model, opt, images, labels, loss
     torch.cuda.empty_cache()
     return out
 
 
-def peak_memory_report(batch=256, k=2, device="cuda", compress_stem=True, time_steps=0):
+def peak_memory_report(batch=256, k=2, device="cuda", compress_stem=True, time_steps=0, head="framework", optimizer="sgd"):
     """The step under each scheme, and the reduction of the peak against scheme "full"."""
-    runs = {s: training_step(s, batch, k, device, compress_stem=compress_stem, time_steps=time_steps) for s in SCHEMES}
+    runs = {s: training_step(s, batch, k, device, compress_stem=compress_stem, time_steps=time_steps, head=head,
+                             optimizer=optimizer) for s in SCHEMES}
     full = runs["full"]["mib"]
-    rep = {"model": "ResNet-50 (53 convolutions), bf16 channels-last, fp32 master weights, SGD momentum",
-           "batch": batch, "k": k, "compress_stem": compress_stem,
+    rep = {"model": "ResNet-50 (53 convolutions), bf16 channels-last, fp32 master weights, "
+                    + ("SGD momentum" if optimizer == "sgd" else "orthogonalised updates, SGD for the rest"),
+           "batch": batch, "k": k, "compress_stem": compress_stem, "head": head, "optimizer": optimizer,
            "points": "Section 3: 1 model, 2 input, 3 forward, 4 after backward, 5 optimizer; MiB above what was "
                      "allocated before the model (torch.cuda.memory_allocated / max_memory_allocated)",
            "schemes": runs}
@@ -290,5 +374,7 @@ if __name__ == "__main__":
     ap.add_argument("--k", type=int, default=2)
     ap.add_argument("--no-stem", action="store_true", help="leave the first convolution uncompressed")
     ap.add_argument("--time-steps", type=int, default=0, help="also time this many further steps per scheme (step_ms)")
+    ap.add_argument("--head", choices=("framework", "fused"), default="framework", help="fused: ac_linear_ce_step")
+    ap.add_argument("--optimizer", choices=("sgd", "muon"), default="sgd", help="muon: ac_muon_update for the convolutions")
     a = ap.parse_args()
-    print(json.dumps(peak_memory_report(a.batch, a.k, "cuda:0", not a.no_stem, a.time_steps), indent=1))
+    print(json.dumps(peak_memory_report(a.batch, a.k, "cuda:0", not a.no_stem, a.time_steps, a.head, a.optimizer), indent=1))
