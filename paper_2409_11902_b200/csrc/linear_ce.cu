@@ -83,7 +83,7 @@ __device__ __forceinline__ float warp_columns(float (&x)[32], int lane) {
 // Statistics of a row's COLS columns; KEEP: and exp(l - m) as fp16.
 template <bool KEEP>
 struct StatsEpi : Ce {
-    static constexpr bool kWholeRow = true;
+    static constexpr bool kWholeRow = true, kSplit = false;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
@@ -133,7 +133,7 @@ struct StatsEpi : Ce {
 
 // g of a piece from its logits and the rows' lse.
 struct GradEpi : Ce {
-    static constexpr bool kWholeRow = true;
+    static constexpr bool kWholeRow = true, kSplit = false;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
@@ -166,13 +166,13 @@ struct GradEpi : Ce {
 
 // A gradient: bf16 to the caller's dense matrix and/or fp32 sums over the pieces.
 struct OutEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true;
     __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
     float* sum;             // [rows][pitch], or null
     const float* top;       // what g was divided by
     int add;                // 1: what earlier pieces left in `sum` is added
     int rows, cols, pitch;
-    __device__ __forceinline__ bool ragged() const { return out && cols % 8 != 0; }
+    __host__ __device__ __forceinline__ bool ragged() const { return out && cols % 8 != 0; }
     __device__ __forceinline__ void store_ragged_patch(float* patch, int lane, int, int row, int col, const float (&v)[4][8]) const {
         store_ragged(out, 0, rows, cols, patch, lane, row, col, v);
     }
@@ -455,7 +455,7 @@ CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
         at += (size_t)up(bytes, 256);
         return o;
     };
-    p.logits = shape(Problem{d.tokens, p.width, d.features, 1, true, false}, true, 0);
+    p.logits = shape(Problem{d.tokens, p.width, d.features, 1, true, false}, true, false, 0);
     p.block = p.logits.bn / 2;
     p.off_top = take(4);
     p.off_stats = take((V + p.block - 1) / p.block * T * 8);

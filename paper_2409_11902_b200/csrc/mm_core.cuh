@@ -12,9 +12,13 @@
 //   CG = 2, BN = 256: a pair of SMs computes a 256 x 256 tile (cta_group::2); each holds 128 rows of A and 128 rows
 //           of B, so a K-tile costs 32 KB of shared memory per SM for twice the MMA work of a lone 128 x 128 tile.
 //   CG = 1, BN = 128 or 64: 128 x 128 or 128 x 64 tiles for problems with fewer than a GPU's worth of large tiles.
-// Where the tiles are too few and K is long, K is cut into slices: each is a tile of its own that leaves fp32 sums in the
-// workspace, and a second kernel adds the slices in their order and applies the epilogue (a cluster that adds them up in
-// distributed shared memory was slower: that memory gives about 25 GB/s to an SM, the L2 three times as much).
+// Where the tiles are too few for the GPU and K is long, K is cut:
+//   SPLIT = 2, 4, 8: a cluster shares a 128 x 128 tile, a part of K each. Every CTA then owns a part of the tile's columns;
+//           it sends the other CTAs their columns of its sums (bulk copies between shared memories), adds what it
+//           receives, in the order of the parts, and applies the epilogue to its columns. Costs about 2.5 us, so it pays
+//           from some 16 K-tiles on. (Reading the sums from the other CTAs' shared memory took 4 us more.)
+//   slices: each is a tile of its own that leaves fp32 sums in the workspace, and a second kernel adds the slices in their
+//           order and applies the epilogue. Any number of slices and any shape of tile, for one launch more.
 // A K-tile of 64 takes an SM 0.27 us in the first shape (its MMAs) and about 0.2 us in the other two; shape() chooses
 // shape and slices by these rates.
 #pragma once
@@ -114,6 +118,12 @@ __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.pr
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                  "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+// From this CTA's shared memory to another's of the cluster (addresses of the cluster's window, but for the source).
+__device__ __forceinline__ void bulk_push(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "r"(src),
+                 "r"(bytes), "r"(bar)
                  : "memory");
 }
 template <int CG>
@@ -237,7 +247,7 @@ __device__ __forceinline__ void store_rows(T* dst, long long pitch, int rows, in
 // ---- the kernel ---------------------------------------------------------------
 
 struct Shared {
-    uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
+    uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2], received;
     uint32_t tmem;
     int abort;
 };
@@ -252,9 +262,10 @@ __device__ __forceinline__ void flag_timeout(int* abort_s, uint32_t* status, uin
 template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { return 128 * 128 + BN / CG * 128; }
 // As many stages as fit (six, eight with 64 columns): the L2 answers a load after about 1.1 us, so the bytes in flight set
 // the rate at which K-tiles arrive.
-template <int CG, int BN> __host__ __device__ constexpr int stage_count() { return 6 * 32768 / stage_bytes<CG, BN>(); }
-template <int CG, int BN, class Epi> __host__ __device__ constexpr int smem_bytes() {
-    return stage_count<CG, BN>() * stage_bytes<CG, BN>() + (Epi::kWholeRow ? kRowPatchBytes : kPatchBytes) + 1024;
+template <int CG, int BN, int SPLIT> __host__ __device__ constexpr int stage_count() { return (SPLIT > 1 ? 5 : 6) * 32768 / stage_bytes<CG, BN>(); }
+template <int CG, int BN, int SPLIT, class Epi> __host__ __device__ constexpr int smem_bytes() {
+    return stage_count<CG, BN, SPLIT>() * stage_bytes<CG, BN>() + 1024 +
+           (SPLIT > 1 ? (SPLIT - 1) * (128 * BN / SPLIT * 4) : Epi::kWholeRow ? kRowPatchBytes : kPatchBytes);
 }
 
 // Tensor memory gives a thread one row; memory wants the threads of a warp side by side along rows. A warp passes 32 x 32
@@ -369,25 +380,89 @@ __device__ __forceinline__ void epilogue_by_patch(const Epi& epi, typename Epi::
     }
 }
 
-template <int CG, int BN, bool AMN, bool BMN, class Epi>
+// The byte offset of column `col` (a multiple of 4) of a row in one CTA's part [128 rows][WIDTH columns] of a split tile.
+template <int WIDTH>
+__device__ __forceinline__ uint32_t part_at(int row, int col) {
+    constexpr int kGroups = WIDTH / 4;
+    return (uint32_t)row * (WIDTH * 4) + (uint32_t)(((col >> 2) ^ (row & (kGroups < 8 ? kGroups - 1 : 7))) << 4);
+}
+
+// The epilogue of a split tile: the 256 threads of warps 4 to 11 of every CTA of the cluster. `got`: the sums are there.
+template <int BN, int SPLIT, class Epi>
+__device__ __forceinline__ void epilogue_split(const Epi& epi, const Tile& tile, uint32_t lanes, uint8_t* own, uint8_t* received,
+                                               uint64_t* bar, uint64_t* tfull, int rank, int tid, int* abort_s, uint32_t* status) {
+    constexpr int kWidth = BN / SPLIT, kRowThreads = kWidth / 8, kStep = 256 / kRowThreads, kRows = 128 / kStep;
+    constexpr uint32_t kPart = 128 * kWidth * 4;
+    const int warp = tid >> 5, lane = tid & 31, quarter = warp & 3, half = (warp - 4) >> 2;
+    const int r = (tid - 128) / kRowThreads, c = (tid - 128) % kRowThreads * 8;      // what this thread finishes
+    const int row = tile.tm * 128 + r, col = tile.tn * BN + rank * kWidth + c;
+    typename Epi::template Ops<kRows> ops;
+    epi.load(ops, tile.batch, row, kStep, col);
+    if (lane == 0 && !mbar_wait(tfull, 0, abort_s)) flag_timeout(abort_s, status, 0x1400u);
+    __syncwarp();
+    tc_fence_after();
+#pragma unroll 1
+    for (int i = 0; i < BN / 2; i += 32) {
+        uint32_t v[32];
+        tmem_ld32(lanes + i, v);
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const int at = half * (BN / 2) + i + j;
+            *reinterpret_cast<uint4*>(own + at / kWidth * kPart + part_at<kWidth>(quarter * 32 + lane, at % kWidth)) =
+                make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        }
+    }
+    fence_proxy_async_smem();
+    bar_sync(1, 256);
+    if (tid == 128) {
+        for (int d = 1; d < SPLIT; ++d) {
+            const int to = (rank + d) % SPLIT, slot = rank < to ? rank : rank - 1;
+            bulk_push(map_rank(smem_u32(received) + slot * kPart, to), smem_u32(own) + to * kPart, kPart, map_rank(smem_u32(bar), to));
+        }
+    }
+    if (lane == 0 && !mbar_wait(bar, 0, abort_s)) flag_timeout(abort_s, status, 0x1700u);
+    __syncwarp();
+    float v[kRows][8] = {};
+#pragma unroll
+    for (int s = 0; s < SPLIT; ++s) {
+        const uint8_t* from = s == rank ? own + rank * kPart : received + (s < rank ? s : s - 1) * kPart;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const float4 a = *reinterpret_cast<const float4*>(from + part_at<kWidth>(r + i * kStep, c));
+            const float4 b = *reinterpret_cast<const float4*>(from + part_at<kWidth>(r + i * kStep, c + 4));
+            v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
+            v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
+        }
+    }
+    epi.apply(ops, tile.batch, row, kStep, col, v);
+}
+
+template <int CG, int BN, bool AMN, bool BMN, int SPLIT, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
 mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb,
           const __grid_constant__ Params p, const __grid_constant__ Epi epi) {
     constexpr int NB = BN / CG;               // rows of B that one CTA holds
     constexpr uint32_t kStage = stage_bytes<CG, BN>();
-    constexpr int kStages = stage_count<CG, BN>();
+    constexpr int kStages = stage_count<CG, BN, SPLIT>();
+    constexpr bool kCluster = CG == 2 || SPLIT > 1;
+    static_assert(SPLIT == 1 || CG == 1, "a cluster is a pair or a split tile");
     extern __shared__ uint8_t smem_raw[];
     __shared__ Shared sh;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
+    const uint32_t rank = kCluster ? cluster_rank() : 0;
+    const int unit = blockIdx.x / (CG * SPLIT), units = gridDim.x / (CG * SPLIT);
     volatile int* abort_flag = &sh.abort;
 
     if (tid == 0) {
         sh.abort = 0;
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(&sh.full[s], 2); mbar_init(&sh.empty[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&sh.tfull[a], 1); mbar_init(&sh.tempty[a], kEpiWarps * CG); }
+        if constexpr (SPLIT > 1) {
+            mbar_init(&sh.received, 1);
+            fence_barrier_init();
+            mbar_arrive_expect_tx(&sh.received, (SPLIT - 1) * (128 * BN / SPLIT * 4));
+        }
         fence_barrier_init();
         prefetch_tmap(&ta);
         prefetch_tmap(&tb);
@@ -395,9 +470,17 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     if (warp == 2) tmem_alloc_cg<CG>(&sh.tmem, 2 * BN);
     tc_fence_before();
     __syncthreads();
-    if constexpr (CG == 2) cluster_sync();
+    if constexpr (kCluster) cluster_sync();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
+    auto tile_of = [&](int t) {
+        Tile tile = decode_tile(p, t);
+        if constexpr (SPLIT > 1) {
+            tile.k0 = p.ktiles * (int)rank / SPLIT;
+            tile.k1 = p.ktiles * ((int)rank + 1) / SPLIT;
+        }
+        return tile;
+    };
     pdl_launch_dependents();
     if (p.reset_status && blockIdx.x == 0 && tid == 64) {
         pdl_wait();
@@ -415,10 +498,10 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             constexpr uint32_t kBytesA = 128 * 128, kBytesB = NB * 128;
             int it = 0;
             bool ok = true;
-            Tile tile = decode_tile(p, unit);
+            Tile tile = tile_of(unit);
             pdl_wait();
             for (int t = unit; t < p.tiles && ok; t += units) {
-                if (t != unit) tile = decode_tile(p, t);
+                if (t != unit) tile = tile_of(t);
                 const int at = is_a ? tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) : tile.tn * BN + (CG == 2 ? (int)rank * NB : 0);
                 const bool skip = !is_a && p.same && tile.tm == tile.tn;      // B's rows are A's
                 const int matrix = tile.batch % p.batch;
@@ -460,7 +543,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             bool ok = true;
             for (int t = unit; t < p.tiles && ok; t += units, ++n) {
                 const int acc = n & 1;
-                const Tile tile = decode_tile(p, t);
+                const Tile tile = tile_of(t);
                 if (!mbar_wait(&sh.tempty[acc], ((n >> 1) & 1) ^ 1, abort_flag)) {
                     flag_timeout(&sh.abort, p.status, 0x1200u + acc);
                     break;
@@ -492,8 +575,12 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         const int quarter = warp & 3, half = (warp - 4) >> 2;       // the TMEM lanes this warp may read; its columns
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * (BN / 2);
         pdl_wait();
+        uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
+        if constexpr (SPLIT > 1)       // the sums replace the stages, which are free once the products are complete
+            epilogue_split<BN, SPLIT>(epi, tile_of(unit), lanes, ring, ring + kStages * kStage, &sh.received, &sh.tfull[0],
+                                      (int)rank, tid, &sh.abort, p.status);
         int n = 0;
-        for (int t = unit; t < p.tiles; t += units, ++n) {
+        for (int t = unit; SPLIT == 1 && t < p.tiles; t += units, ++n) {
             const int acc = n & 1;
             const Tile tile = decode_tile(p, t);
             const int row = tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) + quarter * 32;
@@ -507,8 +594,9 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
                 break;
             }
             tc_fence_after();
-            uint8_t* patches = smem_raw + (base - smem_u32(smem_raw)) + kStages * kStage;
-            if constexpr (Epi::kWholeRow) {
+            uint8_t* patches = ring + kStages * kStage;
+            if constexpr (SPLIT > 1) {
+            } else if constexpr (Epi::kWholeRow) {
                 epi.template row<BN / 2>(lanes + acc * BN, row, lane, col, patches + (warp - 4) * 32 * kRowPatch);
             } else {
                 float* patch = reinterpret_cast<float*>(patches) + (warp - 4) * kPatch;
@@ -529,12 +617,12 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if constexpr (kCluster) cluster_sync();
     if (*abort_flag) {      // copies of an abandoned tile may still be in flight: let them land before this CTA ends
         const long long t0 = clock64();
         while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
         __syncthreads();
     }
-    if constexpr (CG == 2) cluster_sync();
     tc_fence_after();
     if (warp == 2) tmem_dealloc_cg<CG>(tmem, 2 * BN);
 }
@@ -543,7 +631,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
 
 // The sums of one slice, fp32, in the workspace: [slice][batch][rows][pitch].
 struct SliceEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false, kSplit = false;
     float* out;
     int rows, pitch;
     template <int R> struct Ops {};
@@ -619,14 +707,16 @@ struct Problem {
 };
 struct Shape {
     int cg, bn;             // 2, 256: tiles of CTA pairs; 1, 128; 1, 64
+    int split;              // CTAs that share a 128 x 128 tile: 1, 2, 4, 8
     int slices;
     bool half;              // compute the tiles on and above the diagonal only and mirror them
 };
-// The shape with the least expected time. whole_row: the epilogue cannot take slices. Slices need slice_bytes of scratch.
-Shape shape(const Problem& q, bool whole_row, size_t scratch_bytes);
+// The shape with the least expected time. whole_row: the epilogue takes neither slices nor split tiles; ragged: no split
+// tiles. Slices need slice_bytes of scratch.
+Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch_bytes);
 size_t slice_bytes(const Problem& q, int slices);
 inline size_t scratch_bytes(const Problem& q) {      // what shape() would like to have
-    const int s = shape(q, false, ~(size_t)0).slices;
+    const int s = shape(q, false, true, ~(size_t)0).slices;
     return s > 1 ? slice_bytes(q, s) : 0;
 }
 
@@ -652,7 +742,7 @@ struct Call {               // what the launches of one call share
     cudaStream_t stream;
 };
 
-template <int CG, int BN, bool AMN, bool BMN, class Epi>
+template <int CG, int BN, bool AMN, bool BMN, int SPLIT, class Epi>
 ac_status launch_one(const Operand& a, const Operand& b, const Problem& q, const Shape& s, Call& call, const Epi& epi) {
     static bool attr_done[64] = {};
     Params p = make_params(q, s, AMN, BMN);
@@ -662,39 +752,47 @@ ac_status launch_one(const Operand& a, const Operand& b, const Problem& q, const
     CUtensorMap ta, tb;
     ac_status rc = make_map(&ta, a, q.bf16, 128);
     if (rc == AC_OK) rc = make_map(&tb, b, q.bf16, BN / CG);
-    auto kernel = mm_kernel<CG, BN, AMN, BMN, Epi>;
-    if (rc == AC_OK) rc = ensure_smem_limit(kernel, smem_bytes<CG, BN, Epi>(), attr_done);
+    auto kernel = mm_kernel<CG, BN, AMN, BMN, SPLIT, Epi>;
+    if (rc == AC_OK) rc = ensure_smem_limit(kernel, smem_bytes<CG, BN, SPLIT, Epi>(), attr_done);
     if (rc != AC_OK) return rc;
-    const int units = p.tiles < kNumSMs / CG ? p.tiles : kNumSMs / CG;
+    constexpr int kSpan = CG * SPLIT;       // CTAs of a cluster; a split tile's cluster takes no second one
+    const int units = SPLIT > 1 || p.tiles < kNumSMs / CG ? p.tiles : kNumSMs / CG;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(units * CG);
+    cfg.gridDim = dim3(units * kSpan);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem_bytes<CG, BN, Epi>();
+    cfg.dynamicSmemBytes = smem_bytes<CG, BN, SPLIT, Epi>();
     cfg.stream = call.stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.x = kSpan;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = CG > 1 ? 2 : 1;
+    cfg.numAttrs = kSpan > 1 ? 2 : 1;
     AC_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, ta, tb, p, epi));
     return AC_OK;
 }
 
 template <bool AMN, bool BMN, class Epi>
 ac_status launch_shaped(const Operand& a, const Operand& b, const Problem& q, const Shape& s, Call& call, const Epi& epi) {
-    if (s.cg == 2) return launch_one<2, 256, AMN, BMN>(a, b, q, s, call, epi);
-    if (s.bn == 64) return launch_one<1, 64, AMN, BMN>(a, b, q, s, call, epi);
-    return launch_one<1, 128, AMN, BMN>(a, b, q, s, call, epi);
+    if (s.cg == 2) return launch_one<2, 256, AMN, BMN, 1>(a, b, q, s, call, epi);
+    if (s.bn == 64) return launch_one<1, 64, AMN, BMN, 1>(a, b, q, s, call, epi);
+    if constexpr (Epi::kSplit) {
+        if (s.split == 2) return launch_one<1, 128, AMN, BMN, 2>(a, b, q, s, call, epi);
+        if (s.split == 4) return launch_one<1, 128, AMN, BMN, 4>(a, b, q, s, call, epi);
+        if (s.split == 8) return launch_one<1, 128, AMN, BMN, 8>(a, b, q, s, call, epi);
+    }
+    return launch_one<1, 128, AMN, BMN, 1>(a, b, q, s, call, epi);
 }
 
 // D = A B^T for operands of one layout pair.
 template <bool AMN, bool BMN, class Epi>
 ac_status launch(const Operand& a, const Operand& b, const Problem& q, Call& call, const Epi& epi) {
-    const Shape s = shape(q, Epi::kWholeRow, call.scratch_bytes);
     if constexpr (!Epi::kWholeRow) {
+        bool ragged = false;
+        if constexpr (Epi::kRagged) ragged = epi.ragged();
+        const Shape s = shape(q, false, ragged, call.scratch_bytes);
         if (s.slices > 1) {
             const int pitch = (q.n + 7) / 8 * 8;
             const SliceEpi slice{static_cast<float*>(call.scratch), q.m, pitch};
@@ -706,8 +804,10 @@ ac_status launch(const Operand& a, const Operand& b, const Problem& q, Call& cal
                                      call.stream, sums, epi));
             return AC_OK;
         }
+        return launch_shaped<AMN, BMN>(a, b, q, s, call, epi);
+    } else {
+        return launch_shaped<AMN, BMN>(a, b, q, shape(q, true, false, 0), call, epi);
     }
-    return launch_shaped<AMN, BMN>(a, b, q, s, call, epi);
 }
 
 }  // namespace mm

@@ -75,9 +75,9 @@ size_t slice_bytes(const Problem& q, int slices) {
 
 // Expected time in us, from measured rates: a K-tile takes a pair 0.27 us, a lone CTA 0.21 us, 0.19 us with 64 columns; the epilogue of a tile
 // 4 us of a pair, 2 us of a lone CTA, 1.2 us with 64 columns, twice that where it is mirrored, hidden behind the next tile's
-// products where there is one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s).
-Shape shape(const Problem& q, bool whole_row, size_t scratch) {
-    Shape best{1, 128, 1, false};
+// products where there is one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s), a split tile 2.5 us.
+Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch) {
+    Shape best{1, 128, 1, 1, false};
     double least = 1e30;
     const int ktiles = ceil_div(q.k, kBK);
     const struct { int cg, bn; double ktile, tail; } kinds[] = {{1, 128, 0.21, 2.0}, {2, 256, 0.27, 4.0}, {1, 64, 0.19, 1.1}};
@@ -95,9 +95,19 @@ Shape shape(const Problem& q, bool whole_row, size_t scratch) {
                 if (s > 1) t += 6.0 + (double)slice_bytes(q, s) * 2 / 5e6;
                 if (t < least * 0.97) {      // the simpler one unless the other is worth it
                     least = t;
-                    best = Shape{kind.cg, kind.bn, s, half != 0};
+                    best = Shape{kind.cg, kind.bn, 1, s, half != 0};
                 }
             }
+        }
+    }
+    // A cluster lies within one of the GPU's groups of 16 to 20 SMs: at most 16 of 8 CTAs, 32 of 4 run at once.
+    if (whole_row || ragged) return best;
+    const long long tiles = (long long)ceil_div(q.m, 128) * ceil_div(q.n, 128) * q.batch;
+    for (int split = 2; split <= 8 && tiles * split <= (split == 2 ? 144 : 128) && split * 2 <= ktiles; split *= 2) {
+        const double t = (double)ktiles / split * 0.21 + 2.5 + 2.0 / split;
+        if (t < least * 0.97) {
+            least = t;
+            best = Shape{1, 128, split, 1, false};
         }
     }
     return best;

@@ -28,7 +28,7 @@ constexpr int kNormBlocks = 2368;    // 16 blocks per SM; each leaves a partial 
 // with D the diagonal, A^2 = O^2 + D O + O D + D^2. The diagonals go to fp32 vectors, zeros take their place in the fp16
 // matrices.
 struct SymEpi {
-    static constexpr bool kWholeRow = false, kMirror = true, kRagged = false;
+    static constexpr bool kWholeRow = false, kMirror = true, kRagged = false, kSplit = true;
     const __half* a;      // null: A from the accumulators
     const float* da;
     __half* out;
@@ -92,7 +92,7 @@ struct SymEpi {
 // the hi term alone while steps remain that would amplify the difference, all of X in the last two.
 template <bool TALL>
 struct StepEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true;
     const __half* hi;
     __half* lo;             // read and written by the same thread
     __half* hi_out;
@@ -101,7 +101,7 @@ struct StepEpi {
     float a, scale, lo_share;
     int rows, cols;
     long long pitch, sym_pitch;
-    __device__ __forceinline__ bool ragged() const { return update && cols % 8 != 0; }
+    __host__ __device__ __forceinline__ bool ragged() const { return update && cols % 8 != 0; }
     __device__ __forceinline__ void store_ragged_patch(float* patch, int lane, int batch, int row, int col, const float (&v)[4][8]) const {
         store_ragged(update, (long long)batch * rows * cols, rows, cols, patch, lane, row, col, v);
     }
