@@ -15,8 +15,8 @@
 // Where the tiles are too few for the GPU and K is long, K is cut:
 //   SPLIT = 2, 4, 8: a cluster shares a 128 x 128 tile, a part of K each. Every CTA then owns a part of the tile's columns;
 //           it sends the other CTAs their columns of its sums (bulk copies between shared memories), adds what it
-//           receives, in the order of the parts, and applies the epilogue to its columns. Costs about 2.5 us, so it pays
-//           from some 16 K-tiles on. (Reading the sums from the other CTAs' shared memory took 4 us more.)
+//           receives, in the order of the parts, and applies the epilogue to its columns. The exchange takes 1 to 2 us, so
+//           it pays from some 16 K-tiles on. (Reading the sums from the other CTAs' shared memory took 4 us more.)
 //   slices: each is a tile of its own that leaves fp32 sums in the workspace, and a second kernel adds the slices in their
 //           order and applies the epilogue. Any number of slices and any shape of tile, for one launch more.
 // A K-tile of 64 takes an SM 0.27 us in the first shape (its MMAs) and about 0.2 us in the other two; shape() chooses

@@ -73,9 +73,13 @@ size_t slice_bytes(const Problem& q, int slices) {
     return (size_t)slices * q.batch * q.m * ((q.n + 7) / 8 * 8) * 4;
 }
 
-// Expected time in us, from measured rates: a K-tile takes a pair 0.27 us, a lone CTA 0.21 us, 0.19 us with 64 columns; the epilogue of a tile
-// 4 us of a pair, 2 us of a lone CTA, 1.2 us with 64 columns, twice that where it is mirrored, hidden behind the next tile's
-// products where there is one; slices cost a launch (6 us) and their sums' way to memory and back (8 bytes per value at 5 TB/s), a split tile 2.5 us.
+// Expected time in us, from measured rates. A K-tile takes a pair 0.27 us, a lone CTA 0.21 us, 0.19 us with 64 columns; the
+// epilogue of a tile 4 us of a pair, 2 us of a lone CTA, 1.1 us with 64 columns, twice that where it is mirrored, hidden
+// behind the next tile's products where there is one. Slices cost a launch (8 us) and their sums' way to memory and back (8
+// bytes per value at 5 TB/s); a split tile its exchange, epilogue included, and more where the GPU is nearly empty, whose
+// kernels otherwise set themselves up behind one another: a cluster is placed later than as many single CTAs. Updates,
+// unsplit and split in two: 8 tiles of 26 K-tiles 115 -> 125 us, 24 tiles of 16 117 -> 134, 45 tiles of 17 185 -> 177,
+// 49 tiles of 25 187 -> 181; 24 tiles of 36 in four 146 -> 144.
 Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch) {
     Shape best{1, 128, 1, 1, false};
     double least = 1e30;
@@ -92,7 +96,7 @@ Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch) {
                 if (s > 1 && slice_bytes(q, s) > scratch) break;
                 const double waves = (double)((tiles * s + units - 1) / units), main = (double)ktiles / s * kind.ktile;
                 double t = waves * (main > tail ? main : tail) + (main > tail ? tail : main);
-                if (s > 1) t += 6.0 + (double)slice_bytes(q, s) * 2 / 5e6;
+                if (s > 1) t += 8.0 + (double)slice_bytes(q, s) * 2 / 5e6;
                 if (t < least * 0.97) {      // the simpler one unless the other is worth it
                     least = t;
                     best = Shape{kind.cg, kind.bn, 1, s, half != 0};
@@ -104,7 +108,7 @@ Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch) {
     if (whole_row || ragged) return best;
     const long long tiles = (long long)ceil_div(q.m, 128) * ceil_div(q.n, 128) * q.batch;
     for (int split = 2; split <= 8 && tiles * split <= (split == 2 ? 144 : 128) && split * 2 <= ktiles; split *= 2) {
-        const double t = (double)ktiles / split * 0.21 + 2.5 + 2.0 / split;
+        const double t = (double)ktiles / split * 0.21 + (split == 2 ? (tiles > 32 ? 3.3 : 6.4) : split == 4 ? 7.0 : 9.0);
         if (t < least * 0.97) {
             least = t;
             best = Shape{1, 128, split, 1, false};

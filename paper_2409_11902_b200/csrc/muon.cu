@@ -74,12 +74,13 @@ struct SymEpi {
         for (int i = 0; i < R; ++i) {
             const int r = row + i * step;
             if (r >= n) return;
+            float diagonal = 0.f;       // one branch for the eight columns
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (r == col + j) {
-                    dout[line + r] = v[i][j];
-                    v[i][j] = 0.f;
-                }
+            for (int j = 0; j < 8; ++j) {
+                diagonal = r == col + j ? v[i][j] : diagonal;
+                v[i][j] = r == col + j ? 0.f : v[i][j];
+            }
+            if ((unsigned)(r - col) < 8u) dout[line + r] = diagonal;
             store8(out + base + r * pitch, v[i]);
         }
     }
