@@ -60,6 +60,10 @@ struct Params {
     uint32_t idesc;
     uint32_t* status;     // status block of the workspace
     int reset_status;     // 1: first launch of the call
+    // Two products of the same inputs side by side. The first lets its successor start only once what precedes it is
+    // complete; the second then need not wait for the first before it starts, but before it ends, so that whatever waits
+    // for the second has waited for both.
+    int first_of_two, second_of_two;
 };
 
 struct Tile {
@@ -481,7 +485,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         }
         return tile;
     };
-    pdl_launch_dependents();
+    if (!p.first_of_two) pdl_launch_dependents();
     if (p.reset_status && blockIdx.x == 0 && tid == 64) {
         pdl_wait();
         p.status[0] = 0u;
@@ -499,7 +503,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             int it = 0;
             bool ok = true;
             Tile tile = tile_of(unit);
-            pdl_wait();
+            if (!p.second_of_two) pdl_wait();
             for (int t = unit; t < p.tiles && ok; t += units) {
                 if (t != unit) tile = tile_of(t);
                 const int at = is_a ? tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) : tile.tn * BN + (CG == 2 ? (int)rank * NB : 0);
@@ -574,7 +578,8 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         // ------------------------------------------------------------- epilogue
         const int quarter = warp & 3, half = (warp - 4) >> 2;       // the TMEM lanes this warp may read; its columns
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * (BN / 2);
-        pdl_wait();
+        if (!p.second_of_two) pdl_wait();
+        if (p.first_of_two && tid == 128) pdl_launch_dependents();
         uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
         if constexpr (SPLIT > 1)       // the sums replace the stages, which are free once the products are complete
             epilogue_split<BN, SPLIT>(epi, tile_of(unit), lanes, ring, ring + kStages * kStage, &sh.received, &sh.tfull[0],
@@ -617,6 +622,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (p.second_of_two) pdl_wait();
     if constexpr (kCluster) cluster_sync();
     if (*abort_flag) {      // copies of an abandoned tile may still be in flight: let them land before this CTA ends
         const long long t0 = clock64();
@@ -715,6 +721,8 @@ struct Shape {
 // tiles. Slices need slice_bytes of scratch.
 Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch_bytes);
 size_t slice_bytes(const Problem& q, int slices);
+// Whether two products' CTAs fit the GPU side by side, and neither needs the scratch for slices.
+bool fit_together(const Problem& a, const Problem& b, bool ragged, size_t scratch_bytes);
 inline size_t scratch_bytes(const Problem& q) {      // what shape() would like to have
     const int s = shape(q, false, true, ~(size_t)0).slices;
     return s > 1 ? slice_bytes(q, s) : 0;
@@ -740,6 +748,7 @@ struct Call {               // what the launches of one call share
     void* scratch;          // for slices
     size_t scratch_bytes;
     cudaStream_t stream;
+    int of_two;             // 1, 2: the next launch is the first, second of two side by side
 };
 
 template <int CG, int BN, bool AMN, bool BMN, int SPLIT, class Epi>
@@ -749,6 +758,8 @@ ac_status launch_one(const Operand& a, const Operand& b, const Problem& q, const
     p.status = call.status;
     p.reset_status = call.reset;
     call.reset = false;
+    p.first_of_two = call.of_two == 1;
+    p.second_of_two = call.of_two == 2;
     CUtensorMap ta, tb;
     ac_status rc = make_map(&ta, a, q.bf16, 128);
     if (rc == AC_OK) rc = make_map(&tb, b, q.bf16, BN / CG);

@@ -117,5 +117,15 @@ Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch) {
     return best;
 }
 
+bool fit_together(const Problem& a, const Problem& b, bool ragged, size_t scratch_bytes) {
+    long long ctas = 0;
+    for (const Problem* q : {&a, &b}) {
+        const Shape s = shape(*q, false, ragged, scratch_bytes);
+        if (s.slices > 1) return false;
+        ctas += (long long)make_params(*q, s, false, false).tiles * s.cg * s.split;
+    }
+    return ctas <= kNumSMs;
+}
+
 }  // namespace mm
 }  // namespace ac

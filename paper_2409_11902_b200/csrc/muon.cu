@@ -419,7 +419,7 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
         return AC_OK;
     }
     const bool tall = d.rows > d.cols;
-    Call call{status, false, ws + p.off_slices, p.slice_bytes, st};
+    Call call{status, false, ws + p.off_slices, p.slice_bytes, st, 0};
     const Problem qa = gram_problem(d), qp = square_problem(d), qx = step_problem(d);
     const long long x_stride = (long long)d.rows * p.pitch, s_stride = (long long)p.k * p.sym_pitch;
     for (int i = 0; i < d.steps; ++i) {
