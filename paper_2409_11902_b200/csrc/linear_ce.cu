@@ -53,12 +53,28 @@ __device__ __forceinline__ void logits32(const Ce& c, uint32_t taddr, int col, f
 #pragma unroll
     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
     if (c.bias) {
-        const __nv_bfloat16* b = c.bias + c.first;       // clamped, not guarded: guarded loads would wait for one another
-        float add[32];
+        const __nv_bfloat16* b = c.bias + c.first;
+        if (col + 32 <= c.width) {      // 64 bytes, on a boundary of 64
+            uint4 u[4];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) add[j] = __bfloat162float(b[min(col + j, c.width - 1)]);
+            for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const uint4*>(b + col + 8 * j);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] += add[j];
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w[4] = {u[j].x, u[j].y, u[j].z, u[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+                    x[8 * j + 2 * i] += f.x;
+                    x[8 * j + 2 * i + 1] += f.y;
+                }
+            }
+        } else {                        // clamped, not guarded: guarded loads would wait for one another
+            float add[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) add[j] = __bfloat162float(b[max(0, min(col + j, c.width - 1))]);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] += add[j];
+        }
     }
     if (col + 32 > c.width) {
 #pragma unroll
@@ -84,11 +100,12 @@ __device__ __forceinline__ float warp_columns(float (&x)[32], int lane) {
 // Statistics of a row's COLS columns; KEEP: and exp(l - m) as fp16.
 template <bool KEEP>
 struct StatsEpi : Ce {
-    static constexpr bool kWholeRow = true, kSplit = false;
+    static constexpr bool kWholeRow = true, kSplit = false, kTwo = false;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
     __device__ __forceinline__ void row(uint32_t taddr, int row0, int lane, int col, uint8_t* patch) const {
+        if (row0 >= tokens || col >= pitch) return;      // the whole warp
         const int t = row0 + lane;
         const bool in = t < tokens;
         const int label = [&] {
@@ -134,11 +151,12 @@ struct StatsEpi : Ce {
 
 // g of a piece from its logits and the rows' lse.
 struct GradEpi : Ce {
-    static constexpr bool kWholeRow = true, kSplit = false;
+    static constexpr bool kWholeRow = true, kSplit = false, kTwo = false;
     template <int R> struct Ops {};
     template <int R> __device__ __forceinline__ void load(Ops<R>&, int, int, int, int) const {}
     template <int COLS>
     __device__ __forceinline__ void row(uint32_t taddr, int row0, int lane, int col, uint8_t* patch) const {
+        if (row0 >= tokens || col >= pitch) return;      // the whole warp
         const int t = row0 + lane;
         const bool in = t < tokens;
         const long long y = in ? labels[t] : -1;
@@ -172,7 +190,7 @@ struct GradEpi : Ce {
 
 // A gradient: bf16 to the caller's dense matrix and/or fp32 sums over the pieces.
 struct OutEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true, kTwo = true;
     __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
     float* sum;             // [rows][pitch], or null
     const float* top;       // what g was divided by

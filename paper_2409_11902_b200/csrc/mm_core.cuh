@@ -485,7 +485,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         }
         return tile;
     };
-    if (!p.first_of_two) pdl_launch_dependents();
+    if (!Epi::kTwo || !p.first_of_two) pdl_launch_dependents();
     if (p.reset_status && blockIdx.x == 0 && tid == 64) {
         pdl_wait();
         p.status[0] = 0u;
@@ -503,7 +503,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
             int it = 0;
             bool ok = true;
             Tile tile = tile_of(unit);
-            if (!p.second_of_two) pdl_wait();
+            if (!Epi::kTwo || !p.second_of_two) pdl_wait();
             for (int t = unit; t < p.tiles && ok; t += units) {
                 if (t != unit) tile = tile_of(t);
                 const int at = is_a ? tile.tm * (128 * CG) + (CG == 2 ? (int)rank * 128 : 0) : tile.tn * BN + (CG == 2 ? (int)rank * NB : 0);
@@ -578,8 +578,8 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
         // ------------------------------------------------------------- epilogue
         const int quarter = warp & 3, half = (warp - 4) >> 2;       // the TMEM lanes this warp may read; its columns
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * (BN / 2);
-        if (!p.second_of_two) pdl_wait();
-        if (p.first_of_two && tid == 128) pdl_launch_dependents();
+        if (!Epi::kTwo || !p.second_of_two) pdl_wait();
+        if (Epi::kTwo && p.first_of_two && tid == 128) pdl_launch_dependents();
         uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
         if constexpr (SPLIT > 1)       // the sums replace the stages, which are free once the products are complete
             epilogue_split<BN, SPLIT>(epi, tile_of(unit), lanes, ring, ring + kStages * kStage, &sh.received, &sh.tfull[0],
@@ -622,7 +622,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (p.second_of_two) pdl_wait();
+    if (Epi::kTwo && p.second_of_two) pdl_wait();
     if constexpr (kCluster) cluster_sync();
     if (*abort_flag) {      // copies of an abandoned tile may still be in flight: let them land before this CTA ends
         const long long t0 = clock64();
@@ -637,7 +637,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
 
 // The sums of one slice, fp32, in the workspace: [slice][batch][rows][pitch].
 struct SliceEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false, kSplit = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false, kSplit = false, kTwo = false;
     float* out;
     int rows, pitch;
     template <int R> struct Ops {};

@@ -28,7 +28,7 @@ constexpr int kNormBlocks = 2368;    // 16 blocks per SM; each leaves a partial 
 // with D the diagonal, A^2 = O^2 + D O + O D + D^2. The diagonals go to fp32 vectors, zeros take their place in the fp16
 // matrices.
 struct SymEpi {
-    static constexpr bool kWholeRow = false, kMirror = true, kRagged = false, kSplit = true;
+    static constexpr bool kWholeRow = false, kMirror = true, kRagged = false, kSplit = true, kTwo = false;
     const __half* a;      // null: A from the accumulators
     const float* da;
     __half* out;
@@ -93,7 +93,7 @@ struct SymEpi {
 // the hi term alone while steps remain that would amplify the difference, all of X in the last two.
 template <bool TALL>
 struct StepEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true, kTwo = false;
     const __half* hi;
     __half* lo;             // read and written by the same thread
     __half* hi_out;
@@ -332,10 +332,17 @@ MuonPlan plan_muon(const ac_muon_desc& d) {
     MuonPlan p{};
     p.k = d.rows < d.cols ? d.rows : d.cols;
     const int l = d.rows < d.cols ? d.cols : d.rows, all = (l + 63) / 64;
-    if (p.k <= kOnchipK && l <= kOnchipL) {
+    if (p.k <= kOnchipK) {
         // as many CTAs as there may be: a slab of 64 columns costs 1.1 us per step, another CTA's sums 0.3 us
-        p.slabs = (all + kOnchipCluster - 1) / kOnchipCluster;
-        p.ctas = (all + p.slabs - 1) / p.slabs;
+        for (int c = all < kOnchipCluster ? all : kOnchipCluster; c > 0 && !p.ctas; --c) {
+            const int slabs = (all + c - 1) / c;
+            if (slabs <= (p.k <= 32 ? 5 : 3) && onchip_bytes(p.k, slabs, (all + slabs - 1) / slabs) <= kOnchipRoom) {
+                p.slabs = slabs;
+                p.ctas = (all + slabs - 1) / slabs;
+            }
+        }
+    }
+    if (p.ctas) {
         p.off_partial = kStatusBlockBytes;
         p.off_hi[0] = p.off_partial + (size_t)up((long long)d.batch * p.ctas * 4, 256);
         p.bytes = p.off_hi[0] + (size_t)(2 * d.batch * p.ctas * up(p.k, 32) * up(p.k, 32) * 4);
@@ -378,7 +385,7 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
     if (p.ctas) {
         static bool attr_done[64] = {};
-        const ac_status rc = ensure_smem_limit(onchip_kernel, (int)kOnchipSmem, attr_done);
+        const ac_status rc = ensure_smem_limit(onchip_kernel, (int)kOnchipRoom, attr_done);
         if (rc != AC_OK) return rc;
         const Onchip o{grad, v_in, v_out, static_cast<__nv_bfloat16*>(update), reinterpret_cast<float*>(ws + p.off_hi[0]),
                        reinterpret_cast<float*>(ws + p.off_partial), status, d.momentum, d.a, d.b, d.c, d.eps, d.scale,
@@ -386,7 +393,7 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3(p.ctas, d.batch);
         cfg.blockDim = dim3(256);
-        cfg.dynamicSmemBytes = kOnchipSmem;
+        cfg.dynamicSmemBytes = onchip_bytes(p.k, p.slabs, p.ctas);
         cfg.stream = st;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -1,7 +1,8 @@
-// The whole update of a small matrix in one kernel: at most 64 on the shorter side (k), 1344 on the longer (l).
+// The whole update of a small matrix in one kernel: at most 32 on the shorter side (k) and 2560 on the longer (l), or
+// 64 and 1344.
 //
-// A cluster of up to 7 CTAs per matrix; each keeps a slice of at most 192 columns of X (k x l; a matrix with more rows
-// than columns is taken transposed) in shared memory from the gradient to the update, as two fp16 terms. Per step:
+// A cluster of up to 8 CTAs per matrix; each keeps a slice of X (k x l; a matrix with more rows than
+// columns is taken transposed) of at most 192 or 320 columns in shared memory from the gradient to the update, as two fp16 terms. Per step:
 //   Gram sum of the slice (tensor cores) -> partial sums to the workspace -> cluster barrier -> every CTA fetches the
 //   others' (bulk copies) and adds all of them in the order of the slices -> A as two fp16 terms -> A^2
 //   -> P = b A + c A^2 as two terms -> X <- a X + P X.
@@ -9,7 +10,7 @@
 // Gram product, read across them the MN-major operand of P X. Every product is formed from both terms of both operands
 // (hi hi + hi lo + lo hi), about 22 bits: at this size the products are a fourth of the time, and the small matrices'
 // errors do not average out. What bounds it is the chain of 15 products, each with its way through tensor memory and
-// shared memory, and 1.2 us for data that another SM has just written: 64 x 576 takes MEASURED in place of 80 for 17
+// shared memory, and 1.2 us for data that another SM has just written: 64 x 576 takes 43 us in place of 80 for 17
 // launches of the kernels for large matrices. Beyond k = 64 the partial sums are 64 KB each, and their exchange costs
 // more than those launches (128 x 1152: 106 us against 95).
 #pragma once
@@ -22,11 +23,14 @@ using namespace mm;
 
 namespace {
 
-constexpr int kOnchipK = 64, kOnchipSlabs = 3, kOnchipCluster = 7;
-constexpr int kOnchipL = kOnchipSlabs * 64 * kOnchipCluster;
+constexpr int kOnchipK = 64, kOnchipCluster = 8;
 constexpr uint32_t kSlab = 128 * 128;                     // 128 rows of 64 16-bit elements
-constexpr uint32_t kGram = kOnchipK * kOnchipK * 4;          // one slice's partial sums at most
-constexpr uint32_t kOnchipSmem = (2 * kOnchipSlabs + 2) * kSlab + (kOnchipCluster - 1) * kGram + 1024;
+constexpr uint32_t kOnchipRoom = 226 * 1024;               // of an SM's 227 KB; the rest for what is declared in the kernel
+// Shared memory of a CTA: both terms of its slabs of X, both of A and P, the other CTAs' partial sums.
+inline uint32_t onchip_bytes(int k, int slabs, int ctas) {
+    const uint32_t k32 = (k + 31) / 32 * 32;
+    return (2 * slabs + 2) * kSlab + (ctas - 1) * k32 * k32 * 4 + 1024;
+}
 
 template <int W>
 __device__ __forceinline__ void load_grad(const void* grad, int bf16, long long at, float* g) {
@@ -62,7 +66,7 @@ struct Onchip {
     float beta, a, b, c, eps, scale;
     int nesterov, bf16, steps;
     int rows, cols, k, l;
-    int slabs;              // per CTA
+    int slabs;              // per CTA at most
 };
 
 __device__ __forceinline__ uint32_t slab_at(int row, int col) {       // byte offset of an element, 128-byte swizzle
@@ -84,7 +88,7 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
     __shared__ int abort_s;
     __shared__ float part[8];
     uint8_t* smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));
-    uint8_t *xh = smem, *xl = xh + kOnchipSlabs * kSlab, *sh = xl + kOnchipSlabs * kSlab, *sl = sh + kSlab;
+    uint8_t *xh = smem, *xl = xh + p.slabs * kSlab, *sh = xl + p.slabs * kSlab, *sl = sh + kSlab;
     float* others = reinterpret_cast<float*>(sl + kSlab);       // [cluster - 1][k32][k32]
     const uint32_t xh_a = smem_u32(xh), xl_a = smem_u32(xl), sh_a = smem_u32(sh), sl_a = smem_u32(sl);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -103,7 +107,7 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
         fence_barrier_init();
     }
     if (warp == 0) tmem_alloc(&tmem_s, 512);
-    for (uint32_t i = tid * 16; i < 2 * kOnchipSlabs * kSlab; i += 256 * 16)
+    for (uint32_t i = tid * 16; i < 2 * p.slabs * kSlab; i += 256 * 16)
         *reinterpret_cast<uint4*>(xh + i) = make_uint4(0, 0, 0, 0);             // rows past k and columns past l stay zero
     tc_fence_before();
     __syncthreads();
@@ -150,7 +154,7 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
     float sum = 0.f;
     if (p.cols % 4 == 0) {
         // four at a time, and all of a thread's requested before the first is used: u stays in registers
-        constexpr int kQuads = kOnchipK * kOnchipSlabs * 64 / 4 / 256;
+        constexpr int kQuads = 12;       // 64 x 192 or 32 x 320 elements
         float4 u[kQuads];
 #pragma unroll
         for (int q0 = 0; q0 < kQuads; q0 += 6) {
@@ -342,11 +346,13 @@ __global__ void __launch_bounds__(256, 1) onchip_kernel(const __grid_constant__ 
         put();
         // ---- X <- a X + P X
         if (tid == 0) {
-            const uint32_t idesc = idesc0 | (1u << 16) | ((uint32_t)(slabs * 64 >> 3) << 17);
-            for (int s = 0; s < k16 / 16; ++s) {
-                const uint32_t pa = (uint32_t)s * 32, xb = (uint32_t)s * 2048;
-                three(d_x, desc_lo(sh_a + pa, 16), desc_lo(sl_a + pa, 16), desc_lo(xh_a + xb, kSlab), desc_lo(xl_a + xb, kSlab),
-                      idesc, s == 0);
+            for (int g = 0; g < slabs; g += 3) {        // up to 192 columns at a time
+                const uint32_t idesc = idesc0 | (1u << 16) | ((uint32_t)(min(slabs - g, 3) * 64 >> 3) << 17);
+                for (int s = 0; s < k16 / 16; ++s) {
+                    const uint32_t pa = (uint32_t)s * 32, xb = (uint32_t)s * 2048 + g * kSlab;
+                    three(d_x + g * 64, desc_lo(sh_a + pa, 16), desc_lo(sl_a + pa, 16), desc_lo(xh_a + xb, kSlab),
+                          desc_lo(xl_a + xb, kSlab), idesc, s == 0);
+                }
             }
             mma_commit(&done);
         }
