@@ -355,7 +355,7 @@ __device__ __forceinline__ void epilogue_by_patch(const Epi& epi, typename Epi::
     const int pr = lane >> 2, pc = (lane & 3) * 8;
     uint32_t r[32];
     tmem_ld32_issue(taddr, r);
-#pragma unroll 2
+#pragma unroll 1
     for (int c = 0; c < COLS; c += 32) {
         tmem_ld_wait();
 #pragma unroll
