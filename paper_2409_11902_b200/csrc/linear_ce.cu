@@ -15,6 +15,8 @@
 // g is kept divided by the largest |dloss|, which the gradients' epilogues multiply in again: with the weights of a mean
 // the entry of almost every label is close to -1 / count, and rounding that same number to bf16 over and over would bias
 // the sums (backward at 4096 x 65536: 3.0e-3 off; divided 2.2e-3, the two roundings' own share).
+#include <algorithm>
+
 #include "mm_core.cuh"
 
 namespace ac {
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(256) join_kernel(Ce c, int blocks, float* lse,
 }
 
 // The kept piece: g = dloss exp(l - m) exp(m - lse), in place over e; the label's entry from its own fp32 logit. A block
-// takes 32 rows of 256 columns. JOIN: few tokens and classes, so every block joins its rows' statistics itself.
+// takes 32 rows, 256 columns at a time. JOIN: few tokens and classes, so every block joins its rows' statistics itself.
 constexpr int kJoinTokens = 1024, kJoinClasses = 4096;
 template <bool JOIN>
 __global__ void __launch_bounds__(256) kept_kernel(Ce c, int blocks, float* lse_out, float* loss_out, __nv_bfloat16* dbias) {
@@ -316,7 +318,7 @@ __global__ void __launch_bounds__(256) kept_kernel(Ce c, int blocks, float* lse_
     __shared__ int row_label[32];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row0 = blockIdx.x * 32, col = blockIdx.y * 256 + lane * 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row0 = blockIdx.x * 32;
     float top;
     if constexpr (JOIN) {
         top = largest_weight(c.dloss, c.labels, c.tokens, c.classes);
@@ -372,45 +374,49 @@ __global__ void __launch_bounds__(256) kept_kernel(Ce c, int blocks, float* lse_
         row_label[lane] = label;
     }
     __syncthreads();
-    float add[8] = {};
-    if (col < c.pitch) {
-        uint4 x[4];
-        float m[4];
-        const int b = min(c.first + col, c.first + c.width - 1) / c.block;
+    for (int col0 = blockIdx.y * 256; col0 < c.pitch; col0 += gridDim.y * 256) {
+        const int col = col0 + lane * 8;
+        float add[8] = {};
+        if (col < c.pitch) {
+            uint4 x[4];
+            float m[4];
+            const int b = min(c.first + col, c.first + c.width - 1) / c.block;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = min(row0 + warp + 8 * i, c.tokens - 1);
-            x[i] = *reinterpret_cast<const uint4*>(c.e + (long long)r * c.pitch + col);
-            m[i] = c.stats[(long long)b * c.tokens + r].x;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int l = warp + 8 * i, r = row0 + l, label = row_label[l];
-            if (r >= c.tokens) continue;
-            const float weight = row_weight[l];
-            const float f = m[i] == -INFINITY ? 0.f : ex2((m[i] - row_lse[l]) * kLog2e) * (1.f / 32768.f) * weight;
-            float v[8];
-            unpack8(x[i], v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = label == -2 || col + j >= c.width ? 0.f : col + j == label ? (row_p[l] - 1.f) * weight : v[j] * f;
-                add[j] += v[j];
+            for (int i = 0; i < 4; ++i) {
+                const int r = min(row0 + warp + 8 * i, c.tokens - 1);
+                x[i] = *reinterpret_cast<const uint4*>(c.e + (long long)r * c.pitch + col);
+                m[i] = c.stats[(long long)b * c.tokens + r].x;
             }
-            store8(c.g + (long long)r * c.pitch + col, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int l = warp + 8 * i, r = row0 + l, label = row_label[l];
+                if (r >= c.tokens) continue;
+                const float weight = row_weight[l];
+                const float f = m[i] == -INFINITY ? 0.f : ex2((m[i] - row_lse[l]) * kLog2e) * (1.f / 32768.f) * weight;
+                float v[8];
+                unpack8(x[i], v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = label == -2 || col + j >= c.width ? 0.f : col + j == label ? (row_p[l] - 1.f) * weight : v[j] * f;
+                    add[j] += v[j];
+                }
+                store8(c.g + (long long)r * c.pitch + col, v);
+            }
         }
-    }
-    if (!c.columns) return;
-    *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(add[0], add[1], add[2], add[3]);
-    *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(add[4], add[5], add[6], add[7]);
-    __syncthreads();
-    const int at = blockIdx.y * 256 + threadIdx.x;
-    if (at < c.width) {
-        float t = sums[0][threadIdx.x];
-        for (int w = 1; w < 8; ++w) t += sums[w][threadIdx.x];
-        if (dbias)       // no other rows
-            dbias[at] = __float2bfloat16(t * top);
-        else
-            c.columns[(long long)blockIdx.x * c.pitch + at] = t;
+        if (!c.columns) continue;
+        __syncthreads();
+        *reinterpret_cast<float4*>(&sums[warp][lane * 8]) = make_float4(add[0], add[1], add[2], add[3]);
+        *reinterpret_cast<float4*>(&sums[warp][lane * 8 + 4]) = make_float4(add[4], add[5], add[6], add[7]);
+        __syncthreads();
+        const int at = col0 + threadIdx.x;
+        if (at < c.width) {
+            float t = sums[0][threadIdx.x];
+            for (int w = 1; w < 8; ++w) t += sums[w][threadIdx.x];
+            if (dbias)       // no other rows
+                dbias[at] = __float2bfloat16(t * top);
+            else
+                c.columns[(long long)blockIdx.x * c.pitch + at] = t;
+        }
     }
 }
 
@@ -620,9 +626,10 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
         piece(i);
         if (forward && i == p.pieces - 1) {
             Ce k = c;
+            const long long across = std::max<long long>(1, 16 * kNumSMs / ((T + 31) / 32));      // about 16 blocks per SM in all
             k.e = reinterpret_cast<__half*>(c.g);
             AC_CUDA_TRY(launch_after(joined ? kept_kernel<true> : kept_kernel<false>,
-                                     dim3((T + 31) / 32, (unsigned)((p.pitch + 255) / 256)), dim3(256), 0, a.st, k, blocks, a.lse,
+                                     dim3((T + 31) / 32, (unsigned)std::min<long long>((p.pitch + 255) / 256, across)), dim3(256), 0, a.st, k, blocks, a.lse,
                                      a.loss, a.dbias && T <= 32 ? static_cast<__nv_bfloat16*>(a.dbias) + c.first : nullptr));
         } else {
             const Operand W{rows_of_w(), D, c.width, Dp, 1, 0, false};
