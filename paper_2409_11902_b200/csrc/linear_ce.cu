@@ -192,7 +192,7 @@ struct GradEpi : Ce {
 
 // A gradient: bf16 to the caller's dense matrix and/or fp32 sums over the pieces.
 struct OutEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true, kTwo = true;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true, kTwo = true, kRounded = true;
     __nv_bfloat16* out;     // [rows][cols], or null while pieces are still to come
     float* sum;             // [rows][pitch], or null
     const float* top;       // what g was divided by
@@ -201,6 +201,21 @@ struct OutEpi {
     __host__ __device__ __forceinline__ bool ragged() const { return out && cols % 8 != 0; }
     __device__ __forceinline__ void store_ragged_patch(float* patch, int lane, int, int row, int col, const float (&v)[4][8]) const {
         store_ragged(out, 0, rows, cols, patch, lane, row, col, v);
+    }
+    // A final result with rows of whole 16-byte groups and nothing to add: rounded before it goes through the patch.
+    __device__ __forceinline__ bool rounded_first() const { return out && !add && cols % 8 == 0; }
+    template <int COLS>
+    __device__ __forceinline__ void store_rounded(uint32_t taddr, int lane, int row, int col, uint8_t* patch) const {
+        const float scale = *top;
+#pragma unroll 1
+        for (int c = 0; c < COLS; c += 32) {
+            uint32_t r[32];
+            tmem_ld32(taddr + c, r);
+            float x[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]) * scale;
+            store_rows(out + (long long)row * cols + col + c, cols, rows - row, cols - col - c, x, patch, lane);
+        }
     }
     template <int R> struct Ops {
         float4 x[R][2];
@@ -273,10 +288,13 @@ __global__ void __launch_bounds__(1024) weight_kernel(Ce c) {
     if (threadIdx.x == 0) *c.top = m;
 }
 
-// Joins a row's statistics: lse and loss. 8 rows per block; 32 threads share a row's blocks of columns. With dloss, one
-// block more finds the largest weight.
+// Joins a row's statistics: lse and loss. ROWS rows per block, whose 256 / ROWS threads each share their blocks of columns: 8
+// for whole sectors of the statistics, 1 where there are too few rows for that many blocks. With dloss, one block more finds
+// the largest weight.
+template <int ROWS>
 __global__ void __launch_bounds__(256) join_kernel(Ce c, int blocks, float* lse, float* loss) {
-    __shared__ float2 part[32][8];
+    constexpr int kSlices = 256 / ROWS;
+    __shared__ float2 part[kSlices][ROWS];
     pdl_launch_dependents();
     pdl_wait();
     if (c.dloss && blockIdx.x == gridDim.x - 1) {
@@ -284,23 +302,29 @@ __global__ void __launch_bounds__(256) join_kernel(Ce c, int blocks, float* lse,
         if (threadIdx.x == 0) *c.top = m;
         return;
     }
-    const int r = threadIdx.x & 7, slice = threadIdx.x >> 3, t = blockIdx.x * 8 + r;
+    const int r = threadIdx.x % ROWS, slice = threadIdx.x / ROWS, t = blockIdx.x * ROWS + r;
     float2 a = make_float2(-INFINITY, 0.f);
     if (t < c.tokens) {
         int b = slice;
-        for (; b + 96 < blocks; b += 128) {
+        for (; b + 3 * kSlices < blocks; b += 4 * kSlices) {
             float2 x[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = c.stats[(long long)(b + 32 * i) * c.tokens + t];
+            for (int i = 0; i < 4; ++i) x[i] = c.stats[(long long)(b + kSlices * i) * c.tokens + t];
 #pragma unroll
             for (int i = 0; i < 4; ++i) join_stats(a, x[i]);
         }
-        for (; b < blocks; b += 32) join_stats(a, c.stats[(long long)b * c.tokens + t]);
+        for (; b < blocks; b += kSlices) join_stats(a, c.stats[(long long)b * c.tokens + t]);
     }
     part[slice][r] = a;
-    __syncthreads();
-    if (threadIdx.x < 8 && t < c.tokens) {
-        for (int w = 1; w < 32; ++w) join_stats(a, part[w][r]);
+#pragma unroll
+    for (int n = kSlices / 2; n > 0; n >>= 1) {
+        __syncthreads();
+        if (slice < n) {
+            join_stats(a, part[slice + n][r]);
+            part[slice][r] = a;
+        }
+    }
+    if (slice == 0 && t < c.tokens) {
         const float l = a.x + logf(a.y);
         lse[t] = l;
         loss[t] = live(c.labels[t], c.classes) ? l - c.at_label[t] : 0.f;
@@ -619,7 +643,8 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
     const int blocks = (V + p.block - 1) / p.block;
     const bool joined = forward && grad && p.pieces == 1 && T <= kJoinTokens && V <= kJoinClasses;     // by kept_kernel
     if (forward && !joined)
-        AC_CUDA_TRY(launch_after(join_kernel, dim3((T + 7) / 8 + (grad ? 1 : 0)), dim3(256), 0, a.st, c, blocks, a.lse, a.loss));
+        AC_CUDA_TRY(launch_after(T < 8 * kNumSMs ? join_kernel<1> : join_kernel<8>,
+                                 dim3((T < 8 * kNumSMs ? T : (T + 7) / 8) + (grad ? 1 : 0)), dim3(256), 0, a.st, c, blocks, a.lse, a.loss));
     if (grad && !forward) AC_CUDA_TRY(launch_after(weight_kernel, dim3(1), dim3(1024), 0, a.st, c));
     if (!grad) return AC_OK;
     for (int i = p.pieces - 1; i >= 0; --i) {

@@ -605,8 +605,16 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
                 epi.template row<BN / 2>(lanes + acc * BN, row, lane, col, patches + (warp - 4) * 32 * kRowPatch);
             } else {
                 float* patch = reinterpret_cast<float*>(patches) + (warp - 4) * kPatch;
-                epilogue_by_patch<BN / 2>(epi, ops, patch, lanes + acc * BN, lane, tile.batch, row, col,
-                                          p.half && tile.tm != tile.tn);
+                bool stored = false;
+                if constexpr (Epi::kRounded) {
+                    if (epi.rounded_first()) {
+                        epi.template store_rounded<BN / 2>(lanes + acc * BN, lane, row, col, reinterpret_cast<uint8_t*>(patch));
+                        stored = true;
+                    }
+                }
+                if (!stored)
+                    epilogue_by_patch<BN / 2>(epi, ops, patch, lanes + acc * BN, lane, tile.batch, row, col,
+                                              p.half && tile.tm != tile.tn);
             }
             tc_fence_before();
             __syncwarp();
@@ -637,7 +645,7 @@ mm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtens
 
 // The sums of one slice, fp32, in the workspace: [slice][batch][rows][pitch].
 struct SliceEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false, kSplit = false, kTwo = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = false, kSplit = false, kTwo = false, kRounded = false;
     float* out;
     int rows, pitch;
     template <int R> struct Ops {};

@@ -28,7 +28,7 @@ constexpr int kNormBlocks = 2368;    // 16 blocks per SM; each leaves a partial 
 // with D the diagonal, A^2 = O^2 + D O + O D + D^2. The diagonals go to fp32 vectors, zeros take their place in the fp16
 // matrices.
 struct SymEpi {
-    static constexpr bool kWholeRow = false, kMirror = true, kRagged = false, kSplit = true, kTwo = false;
+    static constexpr bool kWholeRow = false, kMirror = true, kRagged = false, kSplit = true, kTwo = false, kRounded = false;
     const __half* a;      // null: A from the accumulators
     const float* da;
     __half* out;
@@ -93,7 +93,7 @@ struct SymEpi {
 // the hi term alone while steps remain that would amplify the difference, all of X in the last two.
 template <bool TALL>
 struct StepEpi {
-    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true, kTwo = false;
+    static constexpr bool kWholeRow = false, kMirror = false, kRagged = true, kSplit = true, kTwo = false, kRounded = false;
     const __half* hi;
     __half* lo;             // read and written by the same thread
     __half* hi_out;
