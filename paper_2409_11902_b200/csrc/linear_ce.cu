@@ -202,6 +202,11 @@ struct OutEpi {
     __device__ __forceinline__ void store_ragged_patch(float* patch, int lane, int, int row, int col, const float (&v)[4][8]) const {
         store_ragged(out, 0, rows, cols, patch, lane, row, col, v);
     }
+    __device__ __forceinline__ void store_ragged8(int, int row, int col, const float (&v)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (row < rows && col + j < cols) out[(long long)row * cols + col + j] = __float2bfloat16(v[j]);
+    }
     // A final result with rows of whole 16-byte groups and nothing to add: rounded before it goes through the patch.
     __device__ __forceinline__ bool rounded_first() const { return out && !add && cols % 8 == 0; }
     template <int COLS>

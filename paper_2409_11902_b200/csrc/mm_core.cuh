@@ -666,46 +666,41 @@ struct SliceEpi {
 struct SliceSums {
     const float* in;
     int rows, pitch, slices, batch;
-    int sym;                // tile edge of a symmetric result, else 0: patches left of the diagonal tiles were not computed
 };
 
-// Adds the slices, first to last, and applies the epilogue. A warp per 32 x 32 patch, grid (patches / 8, 1, batch).
+// Adds the slices, first to last, and applies the epilogue. A warp takes 8 rows of 32 columns, 4 threads per row; eight
+// slices' values are requested at a time. Grid (8 x 32 patches / 8, 1, batch).
 template <class Epi>
 __global__ void __launch_bounds__(256) join_slices_kernel(const __grid_constant__ SliceSums p, const __grid_constant__ Epi epi) {
-    __shared__ __align__(16) float patches[Epi::kMirror || Epi::kRagged ? kEpiWarps * kPatch : 4];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, across = (p.pitch + 31) / 32;
-    const long long patch = (long long)blockIdx.x * 8 + warp;
-    const int row = (int)(patch / across) * 32, col = (int)(patch % across) * 32, batch = blockIdx.z;
-    if (row >= p.rows || (p.sym && col / p.sym < row / p.sym)) return;
-    const int r = row + (lane >> 2), c = col + (lane & 3) * 8;
-    typename Epi::template Ops<4> ops;
-    epi.load(ops, batch, r, 8, c);
-    float v[4][8] = {};
-    // rows clamped, not guarded: a guard around load and addition would make the loads wait for one another
+    const int lane = threadIdx.x & 31, across = (p.pitch + 31) / 32;
+    const long long patch = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int row = (int)(patch / across) * 8 + (lane >> 2), col = (int)(patch % across) * 32 + (lane & 3) * 8, batch = blockIdx.z;
+    typename Epi::template Ops<1> ops;
+    epi.load(ops, batch, row, 8, col);
+    float v[1][8] = {};
+    // clamped, not guarded: a guard around load and addition would make the loads wait for one another
     const long long stride = (long long)p.batch * p.rows * p.pitch;
-    const float* from[4];
+    const float* from = p.in + ((long long)batch * p.rows + min(row, p.rows - 1)) * p.pitch + min(col, p.pitch - 8);
+    for (int s = 0; s < p.slices; s += 8) {
+        float4 a[8], b[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        from[i] = p.in + ((long long)batch * p.rows + min(r + i * 8, p.rows - 1)) * p.pitch + min(c, p.pitch - 8);
-#pragma unroll 4
-    for (int s = 0; s < p.slices; ++s) {
+        for (int i = 0; i < 8; ++i) {
+            const float4* q = reinterpret_cast<const float4*>(from + min(s + i, p.slices - 1) * stride);
+            a[i] = q[0];
+            b[i] = q[1];
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 a = *reinterpret_cast<const float4*>(from[i] + s * stride);
-            const float4 b = *reinterpret_cast<const float4*>(from[i] + s * stride + 4);
-            v[i][0] += a.x; v[i][1] += a.y; v[i][2] += a.z; v[i][3] += a.w;
-            v[i][4] += b.x; v[i][5] += b.y; v[i][6] += b.z; v[i][7] += b.w;
+        for (int i = 0; i < 8; ++i) {
+            const bool on = s + i < p.slices;      // past the end: the last slice again, for nothing
+            v[0][0] += on ? a[i].x : 0.f; v[0][1] += on ? a[i].y : 0.f; v[0][2] += on ? a[i].z : 0.f; v[0][3] += on ? a[i].w : 0.f;
+            v[0][4] += on ? b[i].x : 0.f; v[0][5] += on ? b[i].y : 0.f; v[0][6] += on ? b[i].z : 0.f; v[0][7] += on ? b[i].w : 0.f;
         }
     }
-    epi.apply(ops, batch, r, 8, c, v);
-    if constexpr (Epi::kMirror) {
-        if (p.sym && col / p.sym != row / p.sym)
-            store_mirror_patch(epi, patches + warp * kPatch, lane, batch, row, col, v);
-    }
+    epi.apply(ops, batch, row, 8, col, v);
     if constexpr (Epi::kRagged) {
-        if (epi.ragged()) epi.store_ragged_patch(patches + warp * kPatch, lane, batch, row, col, v);
+        if (epi.ragged()) epi.store_ragged8(batch, row, col, v[0]);
     }
 }
 
@@ -723,7 +718,7 @@ struct Shape {
     int cg, bn;             // 2, 256: tiles of CTA pairs; 1, 128; 1, 64
     int split;              // CTAs that share a 128 x 128 tile: 1, 2, 4, 8
     int slices;
-    bool half;              // compute the tiles on and above the diagonal only and mirror them
+    bool half;              // compute the tiles on and above the diagonal only and mirror them; one slice
 };
 // The shape with the least expected time. whole_row: the epilogue takes neither slices nor split tiles; ragged: no split
 // tiles. Slices need slice_bytes of scratch.
@@ -817,8 +812,8 @@ ac_status launch(const Operand& a, const Operand& b, const Problem& q, Call& cal
             const SliceEpi slice{static_cast<float*>(call.scratch), q.m, pitch};
             const ac_status rc = launch_shaped<AMN, BMN>(a, b, q, s, call, slice);
             if (rc != AC_OK) return rc;
-            const SliceSums sums{slice.out, q.m, pitch, s.slices, q.batch, s.half ? s.bn : 0};
-            const long long patches = (long long)((q.m + 31) / 32) * ((pitch + 31) / 32);
+            const SliceSums sums{slice.out, q.m, pitch, s.slices, q.batch};
+            const long long patches = (long long)((q.m + 7) / 8) * ((pitch + 31) / 32);
             AC_CUDA_TRY(launch_after(join_slices_kernel<Epi>, dim3((unsigned)((patches + 7) / 8), 1, q.batch), dim3(256), 0,
                                      call.stream, sums, epi));
             return AC_OK;

@@ -92,7 +92,7 @@ Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch) {
         for (int half = 0; half <= (q.sym ? 1 : 0); ++half) {
             const long long tiles = (half ? tn * (tn + 1) / 2 : tm * tn) * q.batch;
             const double tail = kind.tail * (half ? 2 : 1);
-            for (int s = 1; s <= (whole_row ? 1 : kMaxSlices) && (s == 1 || s * 2 <= ktiles); ++s) {
+            for (int s = 1; s <= (whole_row || half ? 1 : kMaxSlices) && (s == 1 || s * 2 <= ktiles); ++s) {
                 if (s > 1 && slice_bytes(q, s) > scratch) break;
                 const double waves = (double)((tiles * s + units - 1) / units), main = (double)ktiles / s * kind.ktile;
                 double t = waves * (main > tail ? main : tail) + (main > tail ? tail : main);

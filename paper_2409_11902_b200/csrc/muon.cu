@@ -106,6 +106,11 @@ struct StepEpi {
     __device__ __forceinline__ void store_ragged_patch(float* patch, int lane, int batch, int row, int col, const float (&v)[4][8]) const {
         store_ragged(update, (long long)batch * rows * cols, rows, cols, patch, lane, row, col, v);
     }
+    __device__ __forceinline__ void store_ragged8(int batch, int row, int col, const float (&v)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (row < rows && col + j < cols) update[((long long)batch * rows + row) * cols + col + j] = __float2bfloat16(v[j]);
+    }
     template <int R> struct Ops {
         uint4 x[R], y[R];
         float f[R];
