@@ -488,6 +488,9 @@ __global__ void __launch_bounds__(256) pad_kernel(const __nv_bfloat16* src, __nv
 
 inline long long up(long long a, long long b) { return (a + b - 1) / b * b; }
 
+// Elements between the rows of h and w: as the caller has them where TMA takes that, else of copies whose rows start on 128 bytes.
+inline long long row_pitch(long long features) { return features % 8 == 0 ? features : up(features, 64); }
+
 struct CePlan {
     int width, pieces;                      // columns of g held at a time; pieces of the classes
     Shape logits;                           // one for all pieces: half its tiles' width is the statistics' block
@@ -505,12 +508,12 @@ bool valid(const ac_linear_ce_desc* d) {
 // `width` columns of g at a time.
 CePlan plan_for(const ac_linear_ce_desc& d, bool grad, long long width) {
     CePlan p{};
-    const long long T = d.tokens, V = d.classes, D = d.features, Dp = up(D, 8);
+    const long long T = d.tokens, V = d.classes, D = d.features, Dp = row_pitch(D);
     p.pieces = (int)((V + width - 1) / width);
     width = up((V + p.pieces - 1) / p.pieces, 256);
     p.pieces = (int)((V + width - 1) / width);
     p.width = (int)width;
-    p.pitch = up(width < V ? width : V, 8);
+    p.pitch = up(width < V ? width : V, 64);        // rows of g start on 128 bytes, a line of the L2
     size_t at = kStatusBlockBytes;
     auto take = [&](long long bytes) {
         const size_t o = at;
@@ -596,7 +599,7 @@ ac_status run_ce(const Args& a, bool forward, bool grad) {
     char* ws = static_cast<char*>(a.workspace);
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
     const int T = d.tokens, V = d.classes, D = d.features;
-    const long long Dp = up(D, 8);
+    const long long Dp = row_pitch(D);
     const void *h = a.h, *w = a.w;
     Call call{status, true, ws + p.off_slices, p.slice_bytes, a.st, 0};
     if (D != Dp) {

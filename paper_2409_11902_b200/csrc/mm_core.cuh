@@ -723,6 +723,7 @@ struct Shape {
 // The shape with the least expected time. whole_row: the epilogue takes neither slices nor split tiles; ragged: no split
 // tiles. Slices need slice_bytes of scratch.
 Shape shape(const Problem& q, bool whole_row, bool ragged, size_t scratch_bytes);
+inline int slice_pitch(int n) { return (n + 31) / 32 * 32; }
 size_t slice_bytes(const Problem& q, int slices);
 // Whether two products' CTAs fit the GPU side by side, and neither needs the scratch for slices.
 bool fit_together(const Problem& a, const Problem& b, bool ragged, size_t scratch_bytes);
@@ -808,7 +809,7 @@ ac_status launch(const Operand& a, const Operand& b, const Problem& q, Call& cal
         if constexpr (Epi::kRagged) ragged = epi.ragged();
         const Shape s = shape(q, false, ragged, call.scratch_bytes);
         if (s.slices > 1) {
-            const int pitch = (q.n + 7) / 8 * 8;
+            const int pitch = slice_pitch(q.n);
             const SliceEpi slice{static_cast<float*>(call.scratch), q.m, pitch};
             const ac_status rc = launch_shaped<AMN, BMN>(a, b, q, s, call, slice);
             if (rc != AC_OK) return rc;

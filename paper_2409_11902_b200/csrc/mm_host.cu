@@ -70,7 +70,7 @@ Params make_params(const Problem& q, const Shape& s, bool a_mn, bool b_mn) {
 }
 
 size_t slice_bytes(const Problem& q, int slices) {
-    return (size_t)slices * q.batch * q.m * ((q.n + 7) / 8 * 8) * 4;
+    return (size_t)slices * q.batch * q.m * slice_pitch(q.n) * 4;
 }
 
 // Expected time in us, from measured rates. A K-tile takes a pair 0.27 us, a lone CTA 0.21 us, 0.19 us with 64 columns; the
