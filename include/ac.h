@@ -470,7 +470,8 @@ ac_status ac_selftest_bounded_wait(void *workspace, uint64_t limit_cycles, void 
  *   loss, lse out (backward: lse in): [tokens], fp32.
  *   dh, dw, dbias out: OVERWRITTEN, shapes and type of h, w and bias.
  *   workspace : device scratch. ac_linear_ce_workspace_bytes_min is the least that every call accepts (one
- *               piece of 64 MB of g, or of 4096 classes where that is more, and dh in fp32);
+ *               piece of 64 MB of g, or of 4096 classes where that is more, and dh in fp32; or all classes at
+               once, where that takes less);
  *               ac_linear_ce_workspace_bytes has room for g over all classes where that takes 2 GiB at most.
  *               With any size between, the widest pieces that fit are used: fewer pieces are faster.
  * ac_linear_ce_step is forward and backward in one call for callers that know dloss beforehand; it saves

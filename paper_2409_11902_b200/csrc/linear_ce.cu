@@ -557,21 +557,22 @@ long long ample_width(const ac_linear_ce_desc& d) {
     return w < d.classes ? w : d.classes;
 }
 
-// The widest pieces that fit `bytes`.
+// All columns at once may need less than pieces do: one piece needs no dh in fp32.
+CePlan smaller(const CePlan& a, const CePlan& b) { return b.bytes < a.bytes ? b : a; }
+CePlan ample_plan(const ac_linear_ce_desc& d) { return smaller(plan_for(d, true, d.classes), plan_for(d, true, ample_width(d))); }
+CePlan least_plan(const ac_linear_ce_desc& d) { return smaller(ample_plan(d), plan_for(d, true, least_width(d))); }
+
+// The fewest pieces that fit `bytes`.
 bool plan_ce(const ac_linear_ce_desc& d, bool grad, size_t bytes, CePlan* p) {
     *p = plan_for(d, grad, d.classes);
     if (!grad || p->bytes <= bytes) return p->bytes <= bytes;
-    const long long least = least_width(d);
-    *p = plan_for(d, grad, least);
-    if (p->bytes > bytes) return false;
-    // least fits; more pieces of at least `least` columns need less room, so the first that fits is the widest
-    for (int pieces = 2; pieces < p->pieces; ++pieces) {
-        const CePlan q = plan_for(d, grad, (d.classes + pieces - 1) / pieces);
-        if (q.bytes <= bytes) {
-            *p = q;
-            return true;
-        }
+    const CePlan least = least_plan(d);
+    if (least.bytes > bytes) return false;
+    for (int pieces = 2; pieces < least.pieces; ++pieces) {
+        *p = plan_for(d, grad, (d.classes + pieces - 1) / pieces);
+        if (p->bytes <= bytes) return true;
     }
+    *p = least;
     return true;
 }
 
@@ -723,11 +724,11 @@ using namespace ac;
 extern "C" {
 
 size_t ac_linear_ce_workspace_bytes(const ac_linear_ce_desc* desc) {
-    return valid(desc) ? plan_for(*desc, true, ample_width(*desc)).bytes : 0;
+    return valid(desc) ? ample_plan(*desc).bytes : 0;
 }
 
 size_t ac_linear_ce_workspace_bytes_min(const ac_linear_ce_desc* desc) {
-    return valid(desc) ? plan_for(*desc, true, least_width(*desc)).bytes : 0;
+    return valid(desc) ? least_plan(*desc).bytes : 0;
 }
 
 ac_status ac_linear_ce_forward(const ac_linear_ce_desc* desc, const void* h, const void* w, const void* bias,

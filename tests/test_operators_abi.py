@@ -101,3 +101,23 @@ def test_bindings_raise(ac):
     assert e.value.status == ac.api.AC_ERR_INVALID_ARG
     with pytest.raises(ac.AcError):
         ac.ac_linear_ce_forward(ac.LinearCeDesc(8, 8, 8), A, A, None, A, None, A, A, 1 << 20, stream=0)
+
+
+def test_every_call_accepts_the_least_workspace_and_all_above(ac):
+    """Random problems: the least size never exceeds the ample one, and no call refuses a size from there on."""
+    import math
+    import random
+    L, api, rng = ac.api.lib(), ac.api, random.Random(7)
+    size = lambda top: int(math.exp(rng.uniform(0, math.log(top))))  # noqa: E731
+    for _ in range(1500):
+        d = ac.LinearCeDesc(size(70000), size(300000), size(9000), bias=rng.random() < 0.5)
+        c = d.c()
+        b = A if d.bias else None
+        least, ample = ac.ac_linear_ce_workspace_bytes_min(d), ac.ac_linear_ce_workspace_bytes(d)
+        assert 0 < least <= ample, d
+        if api.torch.cuda.is_available():
+            continue        # the addresses below are not memory: without a GPU the calls end at the first launch
+        assert L.ac_linear_ce_forward(ctypes.byref(c), A, A, b, A, A, A, A, least, None) == api.AC_ERR_CUDA, d
+        for n in (least, ample, rng.randint(least, ample)):
+            assert L.ac_linear_ce_step(ctypes.byref(c), A, A, b, A, A, A, A, A, A, b, A, n, None) == api.AC_ERR_CUDA, (d, n)
+            assert L.ac_linear_ce_backward(ctypes.byref(c), A, A, b, A, A, A, A, A, b, A, n, None) == api.AC_ERR_CUDA, (d, n)
