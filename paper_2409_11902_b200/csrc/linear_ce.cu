@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(256) join_kernel(Ce c, int blocks, float* lse,
 constexpr int kJoinTokens = 1024, kJoinClasses = 4096;
 template <bool JOIN>
 __global__ void __launch_bounds__(256) kept_kernel(Ce c, int blocks, float* lse_out, float* loss_out, __nv_bfloat16* dbias) {
-    __shared__ float sums[8][256];
+    __shared__ __align__(16) float sums[8][256];
     __shared__ float2 part[8][32];
     __shared__ float row_lse[32], row_weight[32], row_p[32];
     __shared__ int row_label[32];
