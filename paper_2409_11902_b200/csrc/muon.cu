@@ -15,6 +15,7 @@
 // A and P are symmetric: half of their tiles are computed and written
 // twice.
 #include "muon_onchip.cuh"
+#include "muon_square.cuh"
 
 namespace ac {
 
@@ -333,6 +334,16 @@ Problem step_problem(const ac_muon_desc& d) {
     return Problem{d.rows, d.cols, d.rows < d.cols ? d.rows : d.cols, d.batch, false, false};
 }
 
+// CTAs per matrix of the kernel that forms A and P in one launch; 0: two launches. It gives a matrix one CTA (k <= 128) or one
+// pair, so that a long X X^T takes longer than over more CTAs. Five steps, one launch for both and two: 128 x 1152 (18
+// K-tiles) 63 and 81 us, 61 x 1624 x 8 (26) 90 and 107, 128 x 4096 (64) 103 and 92; pairs: 6 x 1024 x 256 (16) 105 and 108,
+// 6 x 256 x 2304 (36) 152 and 135.
+int square_ctas(const ac_muon_desc& d) {
+    const int k = d.rows < d.cols ? d.rows : d.cols, l = d.rows < d.cols ? d.cols : d.rows, ktiles = (l + kBK - 1) / kBK;
+    if (k <= 128) return ktiles <= 40 ? 1 : 0;
+    return k <= 256 && ktiles <= 16 ? 2 : 0;
+}
+
 MuonPlan plan_muon(const ac_muon_desc& d) {
     MuonPlan p{};
     p.k = d.rows < d.cols ? d.rows : d.cols;
@@ -436,13 +447,21 @@ ac_status run_muon(const ac_muon_desc& d, const void* grad, const float* v_in, f
     Call call{status, false, ws + p.off_slices, p.slice_bytes, st, 0};
     const Problem qa = gram_problem(d), qp = square_problem(d), qx = step_problem(d);
     const long long x_stride = (long long)d.rows * p.pitch, s_stride = (long long)p.k * p.sym_pitch;
+    const int square = square_ctas(d);
     for (int i = 0; i < d.steps; ++i) {
         const __half* X = hi[i & 1];
         const Operand Xk{X, d.cols, d.rows, p.pitch, d.batch, x_stride, false}, Xt{X, d.cols, d.rows, p.pitch, d.batch, x_stride, true};
         const Operand Ak{A, p.k, p.k, p.sym_pitch, d.batch, s_stride, false}, Pk{P, p.k, p.k, p.sym_pitch, d.batch, s_stride, false};
         const SymEpi gram{nullptr, nullptr, A, dA, 0.f, 0.f, p.k, p.sym_pitch}, poly{A, dA, P, dP, d.b, d.c, p.k, p.sym_pitch};
-        ac_status rc = tall ? launch<true, true>(Xt, Xt, qa, call, gram) : launch<false, false>(Xk, Xk, qa, call, gram);
-        if (rc == AC_OK) rc = launch<false, false>(Ak, Ak, qp, call, poly);
+        ac_status rc;
+        if (square) {
+            const Square q{P, dP, status, d.b, d.c, p.k, (int)((qa.k + kBK - 1) / kBK), p.sym_pitch};
+            rc = square == 1 ? (tall ? launch_square<1, true>(Xt, q, d.batch, st) : launch_square<1, false>(Xk, q, d.batch, st))
+                             : (tall ? launch_square<2, true>(Xt, q, d.batch, st) : launch_square<2, false>(Xk, q, d.batch, st));
+        } else {
+            rc = tall ? launch<true, true>(Xt, Xt, qa, call, gram) : launch<false, false>(Xk, Xk, qa, call, gram);
+        }
+        if (rc == AC_OK && !square) rc = launch<false, false>(Ak, Ak, qp, call, poly);
         auto step = [&](auto& e, auto&& go) {
             e.hi = X;
             e.lo = lo;

@@ -1,0 +1,257 @@
+// A = X X^T and P = b A + c A^2 of matrices whose shorter side k is at most 128 (CG = 1: a CTA per matrix) or 256 (CG = 2: a
+// pair), in one kernel: A is one tile, so the CTA that accumulated it has all of it, and its square needs no launch of its
+// own. A's rows go from tensor memory to shared memory as the fp16 operand of the square, 64-column slabs of 128-byte rows; in
+// a pair each CTA keeps its 128 rows, which are both its rows of the left operand and its half of the right one. The diagonals
+// are carried in fp32 as everywhere (muon.cu). A itself never leaves the SM. What bounds it is the chain of loads, products and
+// barriers, not a rate: five steps take 52 us for 100 x 300 (two launches: 71), 71 for 20 x 128 x 512 (89), 49 for 2 x 97 x 85
+// (73).
+#pragma once
+
+#include "mm_core.cuh"
+
+namespace ac {
+
+using namespace mm;
+
+namespace {
+
+constexpr int kSquareStages = 8;
+
+struct Square {
+    __half* out;            // P without its diagonal, [batch][k][pitch]
+    float* dout;            // its diagonal, [batch][pitch]
+    uint32_t* status;
+    float b, c;
+    int k, ktiles;
+    long long pitch;
+};
+
+template <int CG> __host__ __device__ constexpr int square_smem() { return (kSquareStages + 2 * CG) * 16384 + kRowPatchBytes + 1024; }
+
+// The wait for what another CTA of the cluster wrote before it arrived.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    const long long t0 = clock64();
+    while (true) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (*abort_flag || clock64() - t0 > kWaitCycles) return false;
+    }
+}
+
+template <int CG, bool MN>
+__global__ void __launch_bounds__(kThreads, 1) square_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ Square p) {
+    constexpr int BN = 128 * CG;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full[kSquareStages], empty[kSquareStages], gram_done, ready, square_done;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_s;
+    __shared__ __align__(16) float diagonal[BN];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, operand = base + kSquareStages * 16384;
+    uint8_t* const operand_p = smem_raw + (operand - smem_u32(smem_raw));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int matrix = blockIdx.x / CG;
+    volatile int* abort_flag = &abort_s;
+
+    if (tid == 0) {
+        abort_s = 0;
+        for (int s = 0; s < kSquareStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        mbar_init(&gram_done, 1);
+        mbar_init(&ready, kEpiWarps * CG);
+        mbar_init(&square_done, 1);
+        fence_barrier_init();
+        prefetch_tmap(&tx);
+    }
+    if (warp == 2) tmem_alloc_cg<CG>(&tmem_s, 2 * BN);
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = tmem_s;
+    pdl_launch_dependents();
+
+    if (warp == 0) {
+        if (elect_one()) {
+            pdl_wait();
+            for (int kt = 0; kt < p.ktiles; ++kt) {
+                const int s = kt % kSquareStages;
+                if (!mbar_wait(&empty[s], ((kt / kSquareStages) & 1) ^ 1, abort_flag)) {
+                    flag_timeout(&abort_s, p.status, 0x1800u + s);
+                    break;
+                }
+                if (rank == 0) mbar_arrive_expect_tx(&full[s], 16384 * CG);
+                uint32_t bar = smem_u32(&full[s]);
+                if constexpr (CG == 2) bar = map_rank(bar, 0);
+                const uint32_t to = base + s * 16384;
+                if constexpr (MN) {
+                    tma_load_3d<CG>(to, &tx, bar, (int)rank * 128, kt * kBK, matrix);
+                    tma_load_3d<CG>(to + 8192, &tx, bar, (int)rank * 128 + 64, kt * kBK, matrix);
+                } else {
+                    tma_load_3d<CG>(to, &tx, bar, kt * kBK, (int)rank * 128, matrix);
+                }
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        if (elect_one()) {
+            const uint32_t hi = desc_hi(1024, 2);
+            // fp16 operands, fp32 sums, BN x BN
+            const uint32_t square = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BN >> 4) << 24);
+            const uint32_t gram = square | (MN ? (1u << 15) | (1u << 16) : 0u);
+            bool ok = true;
+            for (int kt = 0; kt < p.ktiles; ++kt) {
+                const int s = kt % kSquareStages;
+                if (!mbar_wait(&full[s], (kt / kSquareStages) & 1, abort_flag)) {
+                    flag_timeout(&abort_s, p.status, 0x1900u + s);
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t x = desc_lo(base + s * 16384, MN ? 8192 : 16);
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) {
+                    const uint32_t lo = x + kk * (MN ? 128 : 2);
+                    mma_words<CG>(tmem, lo, hi, lo, hi, gram, (uint32_t)(kt > 0 || kk > 0));
+                }
+                commit_cg<CG>(&empty[s]);
+            }
+            if (ok) {
+                commit_cg<CG>(&gram_done);
+                if (!mbar_wait_cluster(&ready, 0, abort_flag)) {
+                    flag_timeout(&abort_s, p.status, 0x1A00u);
+                } else {
+                    tc_fence_after();
+                    for (int s = 0; s < (p.k + 15) / 16; ++s) {
+                        const uint32_t lo = desc_lo(operand + (s >> 2) * 16384 + (s & 3) * 32, 16);
+                        mma_words<CG>(tmem + BN, lo, hi, lo, hi, square, (uint32_t)(s > 0));
+                    }
+                    commit_cg<CG>(&square_done);
+                }
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2, local = quarter * 32 + lane;
+        const int row0 = (int)rank * 128 + quarter * 32, row = row0 + lane, first = half * (BN / 2);
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + first;
+        uint8_t* patch = operand_p + 2 * CG * 16384 + (warp - 4) * 32 * kRowPatch;
+        pdl_wait();
+        if (lane == 0 && !mbar_wait(&gram_done, 0, abort_flag)) flag_timeout(&abort_s, p.status, 0x1B00u);
+        __syncwarp();
+        tc_fence_after();
+        // ---- A: its diagonal to both CTAs, the rest as the square's operand
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+            uint32_t r[32];
+            tmem_ld32(lanes + c, r);
+            if (first + c == row0) {       // the patch that this warp's part of the diagonal runs through
+                float d = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    d = j == lane ? __uint_as_float(r[j]) : d;
+                    r[j] = j == lane ? 0u : r[j];
+                }
+                if constexpr (CG == 2) {
+                    for (int to = 0; to < 2; ++to)
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_rank(smem_u32(&diagonal[row]), to)), "f"(d) : "memory");
+                } else {
+                    diagonal[row] = d;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                const int col = first + c + j;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[j + i]);
+                store8(reinterpret_cast<__half*>(operand_p + (col >> 6) * 16384 + local * 128 + (((col & 63) * 2) ^ ((local & 7) << 4))), v);
+            }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            for (int to = 0; to < CG; ++to) mbar_arrive_cluster(map_rank(smem_u32(&ready), to));
+            if (!mbar_wait_cluster(&ready, 0, abort_flag)) flag_timeout(&abort_s, p.status, 0x1C00u);
+        }
+        __syncwarp();
+        if (lane == 0 && !mbar_wait(&square_done, 0, abort_flag)) flag_timeout(&abort_s, p.status, 0x1D00u);
+        __syncwarp();
+        tc_fence_after();
+        // ---- P = b A + c (O^2 + D O + O D + D^2)
+        const float di = diagonal[row];
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+            uint32_t r[32], q[32];
+            tmem_ld32_issue(lanes + c, r);
+            tmem_ld32_issue(lanes + BN + c, q);
+            tmem_ld_wait();
+            float x[32];
+            const float4* other = reinterpret_cast<const float4*>(&diagonal[first + c]);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 d = other[j / 4];
+                const float dj[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = __uint_as_float(r[j + i]);
+                    x[j + i] = fmaf(p.b, a, p.c * fmaf(di + dj[i], a, __uint_as_float(q[j + i])));
+                }
+            }
+            if (first + c == row0) {
+                float d = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    d = j == lane ? __uint_as_float(q[j]) : d;
+                    x[j] = j == lane ? 0.f : x[j];
+                }
+                if (row < p.k) p.dout[matrix * p.pitch + row] = fmaf(p.b, di, p.c * fmaf(di, di, d));
+            }
+            store_rows(p.out + ((long long)matrix * p.k + row0) * p.pitch + first + c, p.pitch, p.k - row0, (int)p.pitch - first - c, x,
+                       patch, lane);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    if (*abort_flag) {      // copies of abandoned K-tiles may still be in flight: let them land before this CTA ends
+        const long long t0 = clock64();
+        while (clock64() - t0 < (1ll << 22)) __nanosleep(1000);
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == 2) tmem_dealloc_cg<CG>(tmem, 2 * BN);
+}
+
+template <int CG, bool MN>
+ac_status launch_square(const Operand& x, const Square& p, int batch, cudaStream_t st) {
+    static bool attr_done[64] = {};
+    CUtensorMap tx;
+    ac_status rc = make_map(&tx, x, false, 128);
+    if (rc == AC_OK) rc = ensure_smem_limit(square_kernel<CG, MN>, square_smem<CG>(), attr_done);
+    if (rc != AC_OK) return rc;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(batch * CG);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = square_smem<CG>();
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
+    AC_CUDA_TRY(cudaLaunchKernelEx(&cfg, square_kernel<CG, MN>, tx, p));
+    return AC_OK;
+}
+
+}  // namespace
+}  // namespace ac

@@ -139,3 +139,15 @@ def test_an_infinite_or_nan_weight_stays_in_its_row(ac):
     bad[[7, 9]] = True
     assert bool(o["loss"].isfinite().all()) and bool(o["dh"][~bad].isfinite().all())
     assert not bool(o["dh"][7].isfinite().any()) and not bool(o["dh"][9].isfinite().all())
+
+
+# both sides of the kernel that forms X X^T and its polynomial in one launch: the shorter side, the number of K-tiles, a pair's
+# second CTA with few rows or none of the patches full, more matrices than SMs
+@pytest.mark.parametrize("b,m,n", [(1, 65, 2560), (1, 65, 2561), (1, 128, 1152), (1, 129, 1000), (2, 130, 1024), (1, 130, 1025), (3, 256, 700),
+                                   (1, 257, 700), (1, 1024, 255), (4, 1000, 161), (170, 100, 130), (90, 140, 150), (1, 2560, 128), (2, 300, 97)])
+@pytest.mark.parametrize("kind", ["noise", "lowrank"])
+def test_update_with_the_square_in_the_same_launch(ac, kind, b, m, n):
+    grad = mu.matrix(kind, b, m, n, 41)
+    _, want = mu.plain(grad, None, 0.0, False, 5, 1.0, 1e-7)
+    _, got = mu.run(ac, grad, None, momentum=0.0, nesterov=False)
+    mu.check(got, want)
